@@ -277,6 +277,65 @@ int sd2_sparse_drafter_decode(const sd2_model_t* model, const uint16_t* h_in_bf1
                               uint16_t* k_cache_dev, uint16_t* v_cache_dev, int32_t max_pos, double rope_theta,
                               float* h_out_dev, void* workspace_dev, size_t workspace_bytes, void* stream);
 
+/* ------------------------------------------------------------------ several requests at once: packed rows, an 8-bit cache
+ * The attention of a decoder layer for a batch of requests of different lengths, between two of the linears above:
+ *   sd2_sparse_linear (q|k|v) -> sd2_kv8_append -> sd2_prompt_attention (whole prompts) or sd2_kv8_attention (single tokens,
+ *   drafts and chunks against the cache) -> sd2_sparse_linear (o).
+ * Same decoder as sd2_sparse_drafter_decode: half-split rotary embedding, n_heads / n_kv query heads for each key/value head,
+ * scores times 1/sqrt(head_dim), softmax; a position's keys and values are read back as the cache holds them.
+ *
+ * Packed rows: the rows of all sequences of a call stand one behind the other; sequence b owns rows row_start_dev[b] ..
+ * row_start_dev[b + 1] - 1 (device int32 [n_seq + 1], from 0 on, not decreasing, at most n_rows; a sequence may have none).
+ * Rows behind the last sequence's are neither read nor written.  pos0_dev (device int32 [n_seq]): the position of a
+ * sequence's first row.  Both are read by the kernels, not by the host: a captured call serves whatever they hold when it is
+ * replayed.  Values outside these rules give unspecified results, but no access outside the buffers.
+ * n_seq and n_rows (0 .. 2^24) say how large the arrays are; n_rows * n_heads <= 2^30.  With no rows a call does nothing.
+ *
+ * The cache of one layer: slot b belongs to sequence b.
+ *   k_dev, v_dev              device uint8 [n_slots][n_kv][max_pos][head_dim], e4m3 codes (4 exponent bits, bias 7; largest 448; no infinity)
+ *   k_scale_dev, v_scale_dev  device fp32 [n_slots][n_kv][max_pos / SD2_KV8_BLOCK], a power of two for each block of positions
+ * A value is its code times its block's scale.  The scale of a block is the smallest 2^e, e >= -100, for which the largest finite
+ * magnitude among its positions is at most 448 * 2^e; codes are rounded to nearest, ties to even.  When further positions enter a
+ * block and need a larger scale, the codes that are there are rounded to it (none ever returns to a smaller one).  Infinities
+ * and NaN become NaN and do not count for the scale.  A cache needs no initial contents.
+ * head_dim: a multiple of 16, at most 256.  max_pos: a multiple of SD2_KV8_BLOCK, at most 2^20.  n_slots, n_kv, n_heads:
+ * at most 65536, 4096, 4096, and at most 64 query heads for each key/value head.  All pointers 16-byte aligned. */
+#define SD2_KV8_BLOCK 32
+typedef struct sd2_kv8_cache { /* plain descriptor, owned by the caller, no hidden state */
+    uint8_t *k_dev, *v_dev;
+    float *k_scale_dev, *v_scale_dev;
+    int32_t n_slots, n_kv, max_pos, head_dim;
+} sd2_kv8_cache_t;
+int sd2_kv8_cache_init(sd2_kv8_cache_t* cache, uint8_t* k_dev, uint8_t* v_dev, float* k_scale_dev, float* v_scale_dev, int32_t n_slots,
+                       int32_t n_kv, int32_t max_pos, int32_t head_dim);
+
+/* New rows enter the cache.  qkv_dev: fp32 [n_rows][(n_heads + 2 n_kv) head_dim], what the q|k|v linear writes.  Queries and keys
+ * are rotated (angle position * rope_theta^(-2 i / head_dim), computed in 64 bits; rope_theta > 1), all is rounded to bf16 and written
+ * to rows_bf16_dev (same layout); the rounded keys and values go into the cache at their positions.  Rows at positions
+ * outside 0 .. max_pos - 1 are rounded but not stored.  n_seq <= n_slots.  Positions of a slot from the last new row on keep their
+ * codes; what the block of a sequence's first row holds in front of it counts as the sequence's own. */
+int sd2_kv8_append(const sd2_kv8_cache_t* cache, const float* qkv_dev, int32_t n_heads, const int32_t* row_start_dev,
+                   const int32_t* pos0_dev, int32_t n_seq, int32_t n_rows, double rope_theta, uint16_t* rows_bf16_dev, void* stream);
+
+/* Causal attention inside each of the packed sequences (a row attends to the rows of its sequence up to itself), any length.
+ * q_dev, k_dev, v_dev: bf16, row r of head h at [r * stride + h * head_dim]; q_stride >= n_heads * head_dim, kv_stride >= n_kv * head_dim,
+ * multiples of 8, at most 2^24 (the three may lie in one array, as sd2_kv8_append leaves them).  out_bf16_dev: bf16
+ * [n_rows][n_heads * head_dim], what the output linear takes.  fp32 scores, maxima, sums and results; weights are rounded to bf16.
+ * Infinities and NaN reach the rows that attend to them and no others. */
+int sd2_prompt_attention(const uint16_t* q_dev, const uint16_t* k_dev, const uint16_t* v_dev, int64_t q_stride, int64_t kv_stride,
+                         const int32_t* row_start_dev, int32_t n_seq, int32_t n_rows, int32_t n_heads, int32_t n_kv, int32_t head_dim,
+                         uint16_t* out_bf16_dev, void* stream);
+
+/* Attention of new rows over the cache, theirs included (append them first): row i of sequence b attends to positions
+ * 0 .. pos0[b] + i of slot b (positions from max_pos on do not exist; a row at a negative position attends to nothing and its result is
+ * zero).  q_dev, q_stride, out_bf16_dev, arithmetic: as for sd2_prompt_attention.  max_new (1 .. 64): the most rows that a sequence
+ * has; of a sequence with more, the first max_new are computed.  n_seq <= n_slots.  A long history is cut into stretches that
+ * workgroups take side by side; workspace_dev (>= the reported size, contents irrelevant before and after) holds their results. */
+int sd2_kv8_attention_workspace_size(const sd2_kv8_cache_t* cache, int32_t n_heads, int32_t n_seq, int32_t max_new, size_t* bytes_out);
+int sd2_kv8_attention(const sd2_kv8_cache_t* cache, const uint16_t* q_dev, int64_t q_stride, int32_t n_heads,
+                      const int32_t* row_start_dev, const int32_t* pos0_dev, int32_t n_seq, int32_t n_rows, int32_t max_new,
+                      uint16_t* out_bf16_dev, void* workspace_dev, size_t workspace_bytes, void* stream);
+
 /* ------------------------------------------------------------------ LM head with greedy choice
  * The drafter's next-token choice (Eq. 1 with greedy decoding, as in the footnote to Eq. 3): the
  * largest logit of the LM head, the one linear of the drafter that stays dense (Sec. 2.3 prunes

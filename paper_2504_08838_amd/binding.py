@@ -44,6 +44,13 @@ class ModelShape(C.Structure):
                 ("layers", "hidden", "q_out", "kv_out", "inter", "n_heads", "n_kv", "head_dim")]
 
 
+class Kv8Cache(C.Structure):
+    """Descriptor of one layer's 8-bit key/value cache (the tensors stay the caller's)."""
+
+    _fields_ = [(n, C.c_void_p) for n in ("k_dev", "v_dev", "k_scale_dev", "v_scale_dev")] + [
+        (n, C.c_int32) for n in ("n_slots", "n_kv", "max_pos", "head_dim")]
+
+
 class Model:
     """Owns an sd2_model_t*; keeps the descriptors' device tensors alive via ``keep``."""
 
@@ -127,6 +134,11 @@ def lib():
             "sd2_draft_round": (C.c_int, [vp, vp, i32, vp, i32, vp, vp, sz, vp]),
             "sd2_draft_round_status": (C.c_int, [vp, i32, i32, vp, vp]),
             "sd2_prune_magnitude": (C.c_int, [vp, i32, i32, i32, i32, vp]),
+            "sd2_kv8_cache_init": (C.c_int, [C.POINTER(Kv8Cache), vp, vp, vp, vp, i32, i32, i32, i32]),
+            "sd2_kv8_append": (C.c_int, [C.POINTER(Kv8Cache), vp, i32, vp, vp, i32, i32, C.c_double, vp, vp]),
+            "sd2_prompt_attention": (C.c_int, [vp, vp, vp, C.c_int64, C.c_int64, vp, i32, i32, i32, i32, i32, vp, vp]),
+            "sd2_kv8_attention_workspace_size": (C.c_int, [C.POINTER(Kv8Cache), i32, i32, i32, psz]),
+            "sd2_kv8_attention": (C.c_int, [C.POINTER(Kv8Cache), vp, C.c_int64, i32, vp, vp, i32, i32, i32, vp, vp, sz, vp]),
             "sd2_lm_head_workspace_size": (C.c_int, [i32, i32, i32, C.POINTER(sz)]),
             "sd2_lm_head_argmax": (C.c_int, [vp, i32, i32, vp, i32, vp, vp, vp, vp, sz, vp]),
         }
@@ -361,6 +373,41 @@ def sparse_drafter_decode(model, h_in_ptr, k_tok, pos0, k_cache_ptr, v_cache_ptr
                                            C.c_void_p(v_cache_ptr), max_pos, float(rope_theta), C.c_void_p(h_out_ptr),
                                            C.c_void_p(ws_ptr), ws_bytes, C.c_void_p(stream)),
            "sd2_sparse_drafter_decode")
+
+
+KV8_BLOCK = 32  # positions that share a scale
+
+
+def kv8_cache_init(k_ptr, v_ptr, k_scale_ptr, v_scale_ptr, n_slots, n_kv, max_pos, head_dim):
+    """Device pointers of the codes (uint8 [n_slots][n_kv][max_pos][head_dim]) and scales (fp32 [n_slots][n_kv][max_pos / 32])."""
+    c = Kv8Cache()
+    _check(lib().sd2_kv8_cache_init(C.byref(c), C.c_void_p(k_ptr), C.c_void_p(v_ptr), C.c_void_p(k_scale_ptr), C.c_void_p(v_scale_ptr),
+                                    n_slots, n_kv, max_pos, head_dim), "sd2_kv8_cache_init")
+    return c
+
+
+def kv8_append(cache, qkv_ptr, n_heads, row_start_ptr, pos0_ptr, n_seq, n_rows, rope_theta, rows_bf16_ptr, stream=0):
+    _check(lib().sd2_kv8_append(C.byref(cache), C.c_void_p(qkv_ptr), n_heads, C.c_void_p(row_start_ptr), C.c_void_p(pos0_ptr), n_seq, n_rows,
+                                float(rope_theta), C.c_void_p(rows_bf16_ptr), C.c_void_p(stream)), "sd2_kv8_append")
+
+
+def prompt_attention(q_ptr, k_ptr, v_ptr, q_stride, kv_stride, row_start_ptr, n_seq, n_rows, n_heads, n_kv, head_dim, out_ptr, stream=0):
+    """Strides in values; out: bf16 [n_rows][n_heads * head_dim]."""
+    _check(lib().sd2_prompt_attention(C.c_void_p(q_ptr), C.c_void_p(k_ptr), C.c_void_p(v_ptr), q_stride, kv_stride, C.c_void_p(row_start_ptr),
+                                      n_seq, n_rows, n_heads, n_kv, head_dim, C.c_void_p(out_ptr), C.c_void_p(stream)),
+           "sd2_prompt_attention")
+
+
+def kv8_attention_workspace_size(cache, n_heads, n_seq, max_new):
+    n = C.c_size_t(0)
+    _check(lib().sd2_kv8_attention_workspace_size(C.byref(cache), n_heads, n_seq, max_new, C.byref(n)), "sd2_kv8_attention_workspace_size")
+    return n.value
+
+
+def kv8_attention(cache, q_ptr, q_stride, n_heads, row_start_ptr, pos0_ptr, n_seq, n_rows, max_new, out_ptr, ws_ptr, ws_bytes, stream=0):
+    _check(lib().sd2_kv8_attention(C.byref(cache), C.c_void_p(q_ptr), q_stride, n_heads, C.c_void_p(row_start_ptr), C.c_void_p(pos0_ptr), n_seq,
+                                   n_rows, max_new, C.c_void_p(out_ptr), C.c_void_p(ws_ptr), ws_bytes, C.c_void_p(stream)),
+           "sd2_kv8_attention")
 
 
 def draft_round_workspace_size(model, vocab, k):

@@ -1036,6 +1036,104 @@ int sd2_mask_gradient(const sd2_matrix_t* m, void* grad, int32_t grad_is_bf16, v
                : SD2_ERR_HIP;
 }
 
+// ---- several requests at once: packed rows, 8-bit cache
+
+namespace {
+
+int check_heads(int32_t n_heads, int32_t n_kv, int32_t head_dim) {
+    if (n_heads < 1 || n_kv < 1 || n_heads > 4096 || n_kv > 4096 || n_heads % n_kv || n_heads / n_kv > 64) return SD2_ERR_SHAPE;
+    return (head_dim < 16 || head_dim > 256 || head_dim % 16) ? SD2_ERR_SHAPE : SD2_OK;
+}
+
+int check_kv8_cache(const sd2_kv8_cache_t* c) {
+    if (!c || !c->k_dev || !c->v_dev || !c->k_scale_dev || !c->v_scale_dev) return SD2_ERR_NULL;
+    if (c->n_slots < 1 || c->n_slots > 65536 || c->max_pos < SD2_KV8_BLOCK || c->max_pos > (1 << 20) || c->max_pos % SD2_KV8_BLOCK)
+        return SD2_ERR_SHAPE;
+    const int rc = check_heads(c->n_kv, c->n_kv, c->head_dim);
+    if (rc != SD2_OK) return rc;
+    return (aligned16(c->k_dev) && aligned16(c->v_dev) && aligned16(c->k_scale_dev) && aligned16(c->v_scale_dev)) ? SD2_OK : SD2_ERR_BUFFER;
+}
+
+int check_packed(int32_t n_seq, int32_t n_rows, int32_t n_heads) {
+    if (n_seq < 0 || n_seq > 65536 || n_rows < 0 || n_rows > kMaxPackedRows || (int64_t)n_rows * n_heads > (1 << 30)) return SD2_ERR_RANGE;
+    return SD2_OK;
+}
+
+int check_stride(int64_t stride, int32_t heads, int32_t head_dim) {
+    return (stride < (int64_t)heads * head_dim || stride % 8 || stride > (1 << 24)) ? SD2_ERR_SHAPE : SD2_OK;
+}
+
+Kv8Args kv8_args(const sd2_kv8_cache_t* c) { return {c->k_dev, c->v_dev, c->k_scale_dev, c->v_scale_dev, c->n_kv, c->max_pos, c->head_dim}; }
+
+}  // namespace
+
+int sd2_kv8_cache_init(sd2_kv8_cache_t* cache, uint8_t* k, uint8_t* v, float* k_scale, float* v_scale, int32_t n_slots, int32_t n_kv,
+                       int32_t max_pos, int32_t head_dim) {
+    if (!cache) return SD2_ERR_NULL;
+    const sd2_kv8_cache_t c = {k, v, k_scale, v_scale, n_slots, n_kv, max_pos, head_dim};
+    const int rc = check_kv8_cache(&c);
+    if (rc == SD2_OK) *cache = c;
+    return rc;
+}
+
+int sd2_kv8_append(const sd2_kv8_cache_t* cache, const float* qkv, int32_t n_heads, const int32_t* row_start, const int32_t* pos0,
+                   int32_t n_seq, int32_t n_rows, double rope_theta, uint16_t* rows, void* stream) {
+    int rc = check_kv8_cache(cache);
+    if (rc != SD2_OK) return rc;
+    if (!qkv || !row_start || !pos0 || !rows) return SD2_ERR_NULL;
+    if ((rc = check_heads(n_heads, cache->n_kv, cache->head_dim)) != SD2_OK || (rc = check_packed(n_seq, n_rows, n_heads)) != SD2_OK) return rc;
+    if (n_seq > cache->n_slots || !(rope_theta > 1.0) || !std::isfinite(rope_theta)) return SD2_ERR_RANGE;
+    if (!aligned16(qkv) || !aligned16(row_start) || !aligned16(pos0) || !aligned16(rows)) return SD2_ERR_BUFFER;
+    return launch_kv8_append(kv8_args(cache), qkv, n_heads, row_start, pos0, n_seq, n_rows, rope_theta, rows,
+                             static_cast<hipStream_t>(stream)) == hipSuccess
+               ? SD2_OK
+               : SD2_ERR_HIP;
+}
+
+int sd2_prompt_attention(const uint16_t* q, const uint16_t* k, const uint16_t* v, int64_t q_stride, int64_t kv_stride,
+                         const int32_t* row_start, int32_t n_seq, int32_t n_rows, int32_t n_heads, int32_t n_kv, int32_t head_dim,
+                         uint16_t* out, void* stream) {
+    if (!q || !k || !v || !row_start || !out) return SD2_ERR_NULL;
+    int rc = check_heads(n_heads, n_kv, head_dim);
+    if (rc != SD2_OK || (rc = check_packed(n_seq, n_rows, n_heads)) != SD2_OK || (rc = check_stride(q_stride, n_heads, head_dim)) != SD2_OK ||
+        (rc = check_stride(kv_stride, n_kv, head_dim)) != SD2_OK)
+        return rc;
+    if (!aligned16(q) || !aligned16(k) || !aligned16(v) || !aligned16(row_start) || !aligned16(out)) return SD2_ERR_BUFFER;
+    return launch_prompt_attention(q, k, v, q_stride, kv_stride, row_start, n_seq, n_rows, n_heads, n_kv, head_dim, out,
+                                   static_cast<hipStream_t>(stream)) == hipSuccess
+               ? SD2_OK
+               : SD2_ERR_HIP;
+}
+
+static int kv8_attention_check(const sd2_kv8_cache_t* cache, int32_t n_heads, int32_t n_seq, int32_t max_new) {
+    int rc = check_kv8_cache(cache);
+    if (rc != SD2_OK || (rc = check_heads(n_heads, cache->n_kv, cache->head_dim)) != SD2_OK) return rc;
+    return (n_seq < 0 || n_seq > cache->n_slots) ? SD2_ERR_RANGE : check_tokens(max_new);
+}
+
+int sd2_kv8_attention_workspace_size(const sd2_kv8_cache_t* cache, int32_t n_heads, int32_t n_seq, int32_t max_new, size_t* bytes_out) {
+    if (!bytes_out) return SD2_ERR_NULL;
+    const int rc = kv8_attention_check(cache, n_heads, n_seq, max_new);
+    if (rc == SD2_OK) *bytes_out = kv8_plan(n_heads, cache->n_kv, cache->head_dim, n_seq, max_new).bytes;
+    return rc;
+}
+
+int sd2_kv8_attention(const sd2_kv8_cache_t* cache, const uint16_t* q, int64_t q_stride, int32_t n_heads, const int32_t* row_start,
+                      const int32_t* pos0, int32_t n_seq, int32_t n_rows, int32_t max_new, uint16_t* out, void* ws, size_t ws_bytes,
+                      void* stream) {
+    int rc = kv8_attention_check(cache, n_heads, n_seq, max_new);
+    if (rc != SD2_OK) return rc;
+    if (!q || !row_start || !pos0 || !out || !ws) return SD2_ERR_NULL;
+    if ((rc = check_packed(n_seq, n_rows, n_heads)) != SD2_OK || (rc = check_stride(q_stride, n_heads, cache->head_dim)) != SD2_OK) return rc;
+    if (!aligned16(q) || !aligned16(row_start) || !aligned16(pos0) || !aligned16(out) || !aligned16(ws) ||
+        ws_bytes < kv8_plan(n_heads, cache->n_kv, cache->head_dim, n_seq, max_new).bytes)
+        return SD2_ERR_BUFFER;
+    return launch_kv8_attention(kv8_args(cache), q, q_stride, n_heads, row_start, pos0, n_seq, n_rows, max_new, out, ws,
+                                static_cast<hipStream_t>(stream)) == hipSuccess
+               ? SD2_OK
+               : SD2_ERR_HIP;
+}
+
 // ---- LM head with greedy choice
 
 static int lm_head_check(int32_t vocab, int32_t hidden, int32_t k_tok) {

@@ -228,4 +228,30 @@ inline bool dense_stream_attend_ok(int n_heads, int n_out, int k_tok) {
 hipError_t launch_dense_stream_attend_add(const uint16_t* w, const float* qkv, int n_heads, int n_kv, int n_out, int k_tok, float* h,
                                           hipStream_t s);
 
+// ---- key/value cache in 8 bits: e4m3 codes [slots][n_kv][max_pos][head_dim], a power-of-two scale per 32 positions and head.
+// Rows of several sequences: b owns rows row_start[b] .. row_start[b + 1] - 1 and slot b, its first row is position pos0[b].
+constexpr int kKv8Block = 32;
+constexpr int kMaxPackedRows = 1 << 24;
+struct Kv8Args {
+    uint8_t *k, *v;
+    float *k_scale, *v_scale;  // [slots][n_kv][max_pos / 32]
+    int n_kv, max_pos, head_dim;
+};
+hipError_t launch_kv8_append(const Kv8Args& c, const float* qkv, int n_heads, const int32_t* row_start, const int32_t* pos0, int n_seq,
+                             int n_rows, double theta, uint16_t* rows, hipStream_t s);
+struct Kv8Plan {
+    int dim, nr;     // padded head_dim, row tiles of sixteen in a workgroup
+    int want, tiles; // workgroups to aim for and row tiles a sequence can have, for each key/value head
+    uint32_t bound;  // units of work there can be, for each key/value head
+    size_t stat_off, bytes;
+};
+Kv8Plan kv8_plan(int n_heads, int n_kv, int head_dim, int n_seq, int max_new);
+hipError_t launch_kv8_attention(const Kv8Args& c, const uint16_t* q, int64_t q_stride, int n_heads, const int32_t* row_start,
+                                const int32_t* pos0, int n_seq, int n_rows, int max_new, uint16_t* out, void* ws, hipStream_t s);
+
+// causal attention inside each of the packed sequences; strides in values
+hipError_t launch_prompt_attention(const uint16_t* q, const uint16_t* k, const uint16_t* v, int64_t q_stride, int64_t kv_stride,
+                                   const int32_t* row_start, int n_seq, int n_rows, int n_heads, int n_kv, int head_dim, uint16_t* out,
+                                   hipStream_t s);
+
 }  // namespace sd2

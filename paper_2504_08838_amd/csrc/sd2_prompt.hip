@@ -1,0 +1,250 @@
+// libsd2 -- causal attention over whole prompts, packed one behind the other (gfx950).
+//
+// o_i = sum_{j <= i} exp(q_i k_j / sqrt(D) - m_i) v_j / sum_{j <= i} exp(q_i k_j / sqrt(D) - m_i), in one pass over the positions with
+// a running maximum m_i; products on the matrix cores (bf16 in, fp32 sums), maxima and sums in fp32.  Weights are rounded to bf16 for
+// the second product: half a step of a weight, 2^-9 of it, as much as the rounding of the result itself.
+//
+// The rows of a workgroup are (token, query head of the group) pairs in that order: what is read of keys and values serves the whole
+// group, and the diagonal that is computed and masked is a third as wide with three heads a group.  Scores come out transposed
+// (positions by rows), so that a lane holds runs of eight positions of one row -- positions are dealt to the rows of the first product
+// such that they follow one another -- and these are the second product's operand as they stand: weights never leave the registers.
+// Keys and values go from memory into LDS without passing through registers, a tile ahead; their 16-byte pieces are turned within a row
+// by the row's number, which spreads the reads over the banks.
+#include "sd2_internal.h"
+#include "sd2_rows.h"
+
+namespace sd2 {
+
+constexpr int kPromptWaves = 4;
+constexpr int kPromptRows = 32 * kPromptWaves;
+
+typedef float f32x16 __attribute__((ext_vector_type(16)));
+typedef short s16x4 __attribute__((ext_vector_type(4)));
+
+struct PromptArgs {
+    const uint16_t *q, *k, *v;
+    int64_t q_stride, kv_stride;
+    const int32_t* row_start;
+    int n_seq, n_rows, n_kv, rep, head_dim;
+    float scale;  // log2(e) / sqrt(D)
+    uint16_t* out;
+};
+
+// byte offset of 16-byte piece c of row r in a tile: keys are read sixteen rows at a time, values four rows of four pieces
+template <int D>
+__device__ __forceinline__ int key_place(int r, int c) {
+    return 16 * (r * (D / 8) + (c ^ (D == 64 ? (r >> 1) & 7 : r & 15)));
+}
+template <int D>
+__device__ __forceinline__ int val_place(int r, int c) {
+    return 16 * (r * (D / 8) + (c ^ (D == 64 ? 4 * ((r >> 1) & 1) : 4 * (r & 3))));
+}
+
+template <int D>
+__global__ __launch_bounds__(64 * kPromptWaves, D == 256 ? 1 : 2) void prompt_attention_kernel(PromptArgs a) {
+    constexpr int kTile = D == 256 ? 32 : 64, kRb = kTile / 32, kSteps = D / 16, kDb = D / 32, kBytes = kTile * D * 2;
+    constexpr int kCalls = kBytes / (1024 * kPromptWaves);  // requests of a wavefront for a tile of keys (and of values)
+    __shared__ __attribute__((aligned(16))) uint8_t smem[2][2][kBytes];  // [buffer][keys, values]
+    const int tid = threadIdx.x, lane = tid & 63, wave = __builtin_amdgcn_readfirstlane(tid >> 6), n = lane & 31, h = lane >> 5;
+    const int grp = blockIdx.x % a.n_kv, rep = a.rep, hd = a.head_dim;
+    auto tiles_of = [&](int b) { return (uint32_t)(((int64_t)seq_rows(a.row_start, b, a.n_rows).count * rep + kPromptRows - 1) / kPromptRows); };
+    const SeqUnit u = find_unit(blockIdx.x / a.n_kv, a.n_seq, tiles_of);
+    if (u.seq < 0) return;
+    const SeqRows sr = seq_rows(a.row_start, u.seq, a.n_rows);
+    const int n_used = sr.count * rep;
+    // the longest first
+    const int first = kPromptRows * (int)(tiles_of(u.seq) - 1 - u.index), wave_first = first + 32 * wave;
+    const int n_pos = min(first + kPromptRows - 1, n_used - 1) / rep + 1;               // positions that the workgroup's rows attend to
+    const int wave_pos = wave_first < n_used ? min(wave_first + 31, n_used - 1) / rep + 1 : 0, wave_low = wave_first / rep;
+    const uint16_t* kg = a.k + (size_t)sr.start * a.kv_stride + (size_t)grp * hd;
+    const uint16_t* vg = a.v + (size_t)sr.start * a.kv_stride + (size_t)grp * hd;
+
+    if (hd < D) {  // dimensions that the heads do not have: zero, and never written again
+        for (int i = tid; i < 2 * 2 * kBytes / 16; i += 64 * kPromptWaves) reinterpret_cast<u32x4*>(&smem[0][0][0])[i] = u32x4{0, 0, 0, 0};
+        __syncthreads();
+    }
+    // A tile's requests of this lane: rows r0, r0 + kStep, ..., the turned piece of each; no row past the sequence's last.
+    constexpr int kStep = 64 * kPromptWaves / (D / 8);
+    const int r0 = (64 * wave + lane) / (D / 8), c0 = lane % (D / 8);
+    auto request = [&](int base, int buf) __attribute__((always_inline)) {
+        const uint16_t* kb = kg + (size_t)base * a.kv_stride;
+        const uint16_t* vb = vg + (size_t)base * a.kv_stride;
+        const int last = sr.count - 1 - base;
+#pragma unroll
+        for (int i = 0; i < kCalls; ++i) {
+            const int r = r0 + kStep * i, slot = 1024 * (i * kPromptWaves + wave);
+            const uint32_t row = (uint32_t)min(r, last) * (uint32_t)a.kv_stride;
+            const uint32_t kc = (uint32_t)key_place<D>(r, c0) / 2 % D;
+            const uint32_t vc = (uint32_t)val_place<D>(r, c0) / 2 % D;
+            if (kc < (uint32_t)hd)
+                __builtin_amdgcn_global_load_lds((const __attribute__((address_space(1))) void*)(kb + (row + kc)),
+                                                 (__attribute__((address_space(3))) void*)(&smem[buf][0][slot]), 16, 0, 0);
+            if (vc < (uint32_t)hd)
+                __builtin_amdgcn_global_load_lds((const __attribute__((address_space(1))) void*)(vb + (row + vc)),
+                                                 (__attribute__((address_space(3))) void*)(&smem[buf][1][slot]), 16, 0, 0);
+        }
+    };
+    request(0, 0);
+
+    // operand of the scores: row n, dimensions 16 step + 8 h .. + 7 (rows past the last repeat it; never written)
+    const int row = min(wave_first + n, n_used - 1), token = row / rep, head = grp * rep + (row - token * rep);
+    bf16x8 q[kSteps];
+    {
+        const uint16_t* src = a.q + (size_t)(sr.start + token) * a.q_stride + (size_t)head * hd + 8 * h;
+#pragma unroll
+        for (int i = 0; i < kSteps; ++i) {
+            Frag f;
+            f.q = u32x4{0, 0, 0, 0};
+            if (16 * i < hd) f.q = *reinterpret_cast<const u32x4*>(src + 16 * i);
+            q[i] = f.v;
+        }
+    }
+    float m = -3.0e38f, l = 0.f;
+    f32x16 o[kDb];  // dimension 32 db + 8 (i / 4) + 4 h + i % 4 of row n
+#pragma unroll
+    for (int d = 0; d < kDb; ++d)
+#pragma unroll
+        for (int i = 0; i < 16; ++i) o[d][i] = 0.f;
+
+    // where in a tile the lane reads
+    const int key_row = 16 * (n >> 4) + 8 * ((n >> 2) & 1) + 4 * ((n >> 3) & 1) + (n & 3);
+    const int val_row = 8 * h + ((lane & 15) >> 2), val_piece = 2 * ((lane >> 4) & 1) + ((lane & 3) >> 1), val_byte = 8 * (lane & 1);
+
+    int buf = 0, odd_from = 0x7fffffff;
+    for (int base = 0; base < n_pos; base += kTile, buf ^= 1) {
+        __syncthreads();  // the tile is there (the barrier waits for the wavefront's own requests), and nobody reads the other buffer
+        if (base + kTile < n_pos) request(base + kTile, buf ^ 1);
+        if (base >= wave_pos) continue;
+        const uint8_t* kt = smem[buf][0];
+        const uint8_t* vt = smem[buf][1];
+        f32x16 s[kRb];
+#pragma unroll
+        for (int rb = 0; rb < kRb; ++rb) {
+#pragma unroll
+            for (int i = 0; i < 16; ++i) s[rb][i] = 0.f;
+#pragma unroll
+            for (int i = 0; i < kSteps; ++i) {
+                const bf16x8 kf = *reinterpret_cast<const bf16x8*>(kt + key_place<D>(32 * rb + key_row, 2 * i + h));
+                s[rb] = __builtin_amdgcn_mfma_f32_32x32x16_bf16(kf, q[i], s[rb], 0, 0, 0);
+            }
+        }
+        const bool masked = base + kTile - 1 > wave_low;
+        if (masked) {
+#pragma unroll
+            for (int rb = 0; rb < kRb; ++rb)
+#pragma unroll
+                for (int i = 0; i < 16; ++i)  // position 32 rb + 16 (i / 8) + 8 h + i % 8
+                    if (base + 32 * rb + 16 * (i >> 3) + 8 * h + (i & 7) > token) s[rb][i] = -__builtin_inff();
+        }
+        float mx = s[0][0];
+#pragma unroll
+        for (int rb = 0; rb < kRb; ++rb)
+#pragma unroll
+            for (int i = 0; i < 16; ++i) mx = fmaxf(mx, s[rb][i]);
+        mx *= a.scale;
+        // The maximum follows only where a weight could grow past 2^8: sums of weights up to that are as exact as those below 1.
+        if (__any(mx > m + 8.f)) {
+            const float top = fmaxf(m, max_halves(mx)), f = __builtin_amdgcn_exp2f(m - top);
+            m = top;
+            l *= f;
+#pragma unroll
+            for (int d = 0; d < kDb; ++d) o[d] *= f;
+        }
+        bf16x8 p[kRb][2];  // positions 32 rb + 16 j + 8 h .. + 7
+#pragma unroll
+        for (int rb = 0; rb < kRb; ++rb)
+#pragma unroll
+            for (int j = 0; j < 2; ++j) {
+                float w[8];
+                Frag f;
+#pragma unroll
+                for (int e = 0; e < 8; ++e) {
+                    w[e] = __builtin_amdgcn_exp2f(__builtin_fmaf(s[rb][8 * j + e], a.scale, -m));
+                    l += w[e];
+                }
+#pragma unroll
+                for (int e = 0; e < 4; ++e) f.u[e] = pack_bf16(w[2 * e], w[2 * e + 1]);
+                p[rb][j] = f.v;
+            }
+        // operand of eight positions (32 rb + 16 j + 8 h ..) of dimension 32 db + n: two transposing reads of four rows
+        auto values = [&](int d, int rb, int j) __attribute__((always_inline)) {
+            Frag f;
+#pragma unroll
+            for (int e = 0; e < 2; ++e) {
+                const int r = 32 * rb + 16 * j + 4 * e + val_row;
+                const auto* src = (const __attribute__((address_space(3))) uint8_t*)vt + val_place<D>(r, 4 * d + val_piece) + val_byte;
+                const s16x4 x = __builtin_amdgcn_ds_read_tr16_b64_v4i16((__attribute__((address_space(3))) s16x4*)src);
+                reinterpret_cast<s16x4*>(&f)[e] = x;
+            }
+            return f;
+        };
+        if (masked) {
+            // A weight of zero times an infinity or NaN is NaN, also where the row does not attend to the position: from the first tile
+            // on that holds such a value and is not attended to by all rows, values are added at the end, one position after the other.
+            uint32_t largest = 0;
+#pragma unroll
+            for (int i = 0; i < kBytes / 1024; ++i) {
+                const u32x4 x = *reinterpret_cast<const u32x4*>(vt + 1024 * i + 16 * lane);
+#pragma unroll
+                for (int e = 0; e < 4; ++e) largest = max(largest, max((x[e] << 1) & 0xfffe0000u, (x[e] & 0x7fffu) << 17));
+            }
+            if (__any(largest >= 0xff000000u)) odd_from = min(odd_from, base);
+        }
+        if (odd_from > base) {
+#pragma unroll
+            for (int rb = 0; rb < kRb; ++rb)
+#pragma unroll
+                for (int j = 0; j < 2; ++j)
+#pragma unroll
+                    for (int d = 0; d < kDb; ++d) o[d] = __builtin_amdgcn_mfma_f32_32x32x16_bf16(values(d, rb, j).v, p[rb][j], o[d], 0, 0, 0);
+        }
+    }
+#pragma unroll 1
+    for (int pos = odd_from; pos <= token; ++pos) {
+        const uint16_t* key = kg + (size_t)pos * a.kv_stride;
+        const uint16_t* query = a.q + (size_t)(sr.start + token) * a.q_stride + (size_t)head * hd;
+        float dot = 0.f;
+#pragma unroll 1
+        for (int d = 0; d < hd; ++d) dot += bf16_to_f32(query[d]) * bf16_to_f32(key[d]);
+        const float w = __builtin_amdgcn_exp2f(__builtin_fmaf(dot, a.scale, -m));
+        const uint16_t* src = vg + (size_t)pos * a.kv_stride + 4 * h;
+#pragma unroll
+        for (int d = 0; d < kDb; ++d)
+#pragma unroll
+            for (int i = 0; i < 4; ++i) {
+                if (32 * d + 8 * i >= hd) continue;
+                const uint2 x = *reinterpret_cast<const uint2*>(src + 32 * d + 8 * i);
+                o[d][4 * i] += w * __uint_as_float(x.x << 16);
+                o[d][4 * i + 1] += w * __uint_as_float(x.x & 0xffff0000u);
+                o[d][4 * i + 2] += w * __uint_as_float(x.y << 16);
+                o[d][4 * i + 3] += w * __uint_as_float(x.y & 0xffff0000u);
+            }
+    }
+    if (wave_first + n >= n_used) return;
+    const float inv = 1.0f / sum_halves(l);
+    uint16_t* dst = a.out + ((size_t)(sr.start + token) * a.n_kv * rep + head) * hd + 4 * h;
+#pragma unroll
+    for (int d = 0; d < kDb; ++d)
+#pragma unroll
+        for (int i = 0; i < 4; ++i)
+            if (32 * d + 8 * i < hd)
+                *reinterpret_cast<uint2*>(dst + 32 * d + 8 * i) = make_uint2(pack_bf16(o[d][4 * i] * inv, o[d][4 * i + 1] * inv),
+                                                                              pack_bf16(o[d][4 * i + 2] * inv, o[d][4 * i + 3] * inv));
+}
+
+hipError_t launch_prompt_attention(const uint16_t* q, const uint16_t* k, const uint16_t* v, int64_t q_stride, int64_t kv_stride,
+                                   const int32_t* row_start, int n_seq, int n_rows, int n_heads, int n_kv, int head_dim, uint16_t* out,
+                                   hipStream_t s) {
+    if (head_dim < 16 || head_dim > 256 || head_dim % 16) return hipErrorInvalidValue;
+    if (n_rows == 0 || n_seq == 0) return hipSuccess;
+    const int rep = n_heads / n_kv;
+    const PromptArgs a = {q, k, v, q_stride, kv_stride, row_start, n_seq, n_rows, n_kv, rep, head_dim,
+                          (float)(1.4426950408889634 / sqrt((double)head_dim)), out};
+    const dim3 grid((unsigned)(((int64_t)n_rows * rep / kPromptRows + (n_seq < n_rows ? n_seq : n_rows)) * n_kv)), block(64 * kPromptWaves);
+    if (head_dim <= 64) hipLaunchKernelGGL(prompt_attention_kernel<64>, grid, block, 0, s, a);
+    else if (head_dim <= 128) hipLaunchKernelGGL(prompt_attention_kernel<128>, grid, block, 0, s, a);
+    else hipLaunchKernelGGL(prompt_attention_kernel<256>, grid, block, 0, s, a);
+    return hipGetLastError();
+}
+
+}  // namespace sd2

@@ -329,7 +329,7 @@ int sd2_prompt_attention(const uint16_t* q_dev, const uint16_t* k_dev, const uin
 /* Attention of new rows over the cache, theirs included (append them first): row i of sequence b attends to positions
  * 0 .. pos0[b] + i of slot b (positions from max_pos on do not exist; a row at a negative position attends to nothing and its result is
  * zero).  q_dev, q_stride, out_bf16_dev, arithmetic: as for sd2_prompt_attention.  max_new (1 .. 64): the most rows that a sequence
- * has; of a sequence with more, the first max_new are computed.  n_seq <= n_slots.  A long history is cut into stretches that
+ * has; of a sequence with more, the first max_new are computed.  n_seq <= n_slots, n_seq * max_new * n_heads <= 2^30.  A long history is cut into stretches that
  * workgroups take side by side; workspace_dev (>= the reported size, contents irrelevant before and after) holds their results. */
 int sd2_kv8_attention_workspace_size(const sd2_kv8_cache_t* cache, int32_t n_heads, int32_t n_seq, int32_t max_new, size_t* bytes_out);
 int sd2_kv8_attention(const sd2_kv8_cache_t* cache, const uint16_t* q_dev, int64_t q_stride, int32_t n_heads,

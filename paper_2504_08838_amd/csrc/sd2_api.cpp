@@ -1108,7 +1108,8 @@ int sd2_prompt_attention(const uint16_t* q, const uint16_t* k, const uint16_t* v
 static int kv8_attention_check(const sd2_kv8_cache_t* cache, int32_t n_heads, int32_t n_seq, int32_t max_new) {
     int rc = check_kv8_cache(cache);
     if (rc != SD2_OK || (rc = check_heads(n_heads, cache->n_kv, cache->head_dim)) != SD2_OK) return rc;
-    return (n_seq < 0 || n_seq > cache->n_slots) ? SD2_ERR_RANGE : check_tokens(max_new);
+    if (n_seq < 0 || n_seq > cache->n_slots || (rc = check_tokens(max_new)) != SD2_OK) return SD2_ERR_RANGE;
+    return (int64_t)n_seq * max_new * n_heads > (1 << 30) ? SD2_ERR_RANGE : SD2_OK;
 }
 
 int sd2_kv8_attention_workspace_size(const sd2_kv8_cache_t* cache, int32_t n_heads, int32_t n_seq, int32_t max_new, size_t* bytes_out) {

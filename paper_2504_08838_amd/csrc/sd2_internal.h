@@ -241,9 +241,10 @@ hipError_t launch_kv8_append(const Kv8Args& c, const float* qkv, int n_heads, co
                              int n_rows, double theta, uint16_t* rows, hipStream_t s);
 struct Kv8Plan {
     int dim, nr;     // padded head_dim, row tiles of sixteen in a workgroup
-    int want, tiles; // workgroups to aim for and row tiles a sequence can have, for each key/value head
+    int places;      // workgroups that run at the same time, for each key/value head
+    int tiles;       // row tiles that a sequence can have
     uint32_t bound;  // units of work there can be, for each key/value head
-    size_t stat_off, bytes;
+    size_t stat_off, join_off, bytes;
 };
 Kv8Plan kv8_plan(int n_heads, int n_kv, int head_dim, int n_seq, int max_new);
 hipError_t launch_kv8_attention(const Kv8Args& c, const uint16_t* q, int64_t q_stride, int n_heads, const int32_t* row_start,

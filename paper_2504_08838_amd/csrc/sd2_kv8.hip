@@ -3,6 +3,8 @@
 // A block of 32 positions of one head shares a scale, a power of two: a product with it is exact in fp32, bf16 and the matrix
 // instructions, so quantising rounds once, a block that is still open is brought to a larger scale by its exponents alone, and
 // attention applies scales where they cost nothing (keys: to the score; values: in the conversion to bf16).
+#include <atomic>
+
 #include "sd2_internal.h"
 #include "sd2_rows.h"
 
@@ -67,10 +69,10 @@ __global__ __launch_bounds__(256) void kv8_append_kernel(AppendArgs a) {
     static_assert(kBlock == 32, "shifts by 5");
     __shared__ uint32_t largest[2];
     const int tid = threadIdx.x, grp = blockIdx.y, D = a.c.head_dim, half = D / 2;
-    const SeqUnit u = find_unit(blockIdx.x, a.n_seq, [&](int b) { return touched_blocks(a.pos0[b], seq_rows(a.row_start, b, a.n_rows).count); });
+    const SeqUnit u = Sequences(a.row_start, a.pos0, a.n_seq, a.n_rows).find(blockIdx.x, [](const SeqRows& r) { return touched_blocks(r.pos0, r.count); });
     if (u.seq < 0) return;
-    const SeqRows sr = seq_rows(a.row_start, u.seq, a.n_rows);
-    const int64_t p0 = a.pos0[u.seq], block = (p0 >> 5) + u.index, lo_pos = block * kBlock;
+    const SeqRows sr = u.rows;
+    const int64_t p0 = sr.pos0, block = (p0 >> 5) + u.index, lo_pos = block * kBlock;
     const int64_t first = max(p0, lo_pos);
     const int n_here = (int)(min(p0 + sr.count, lo_pos + kBlock) - first);
     const int row0 = sr.start + (int)(first - p0);
@@ -203,42 +205,54 @@ struct Kv8AttArgs {
     const int32_t* row_start;
     const int32_t* pos0;
     int n_seq, n_rows, max_new, rep;
-    int want;        // workgroups to aim for, for each key/value head
+    int places;      // workgroups that run at the same time, for each key/value head
     uint32_t bound;  // units that the launch and the workspace have room for, for each key/value head
     float scale;     // log2(e) / sqrt(D)
     uint16_t* out;
     float* part;   // [units][key/value heads][16 NR][D]
     float2* stat;  // [units][key/value heads][16 NR]: running maximum (of scores times log2 e) and sum
+    uint2* join;   // [sequences][max_new][query heads]: the row's first unit, and its number of stretches
 };
 
 // How a sequence is cut: row tiles and stretches of positions.  The stretch is the same for all sequences, so that workgroups are
 // about equally long; a sequence's units are its row tiles times its stretches.
 struct SeqCut {
-    int start, count;  // rows
-    int64_t pos0;
-    int n_pos;         // positions that the last of them attends to
+    int count, n_pos;  // rows; positions that the last of them attends to
     uint32_t tiles, spans;
 };
 template <int ROWS>
-__device__ __forceinline__ SeqCut seq_cut(const Kv8AttArgs& a, int b) {
-    const SeqRows sr = seq_rows(a.row_start, b, a.n_rows);
+__device__ __forceinline__ SeqCut seq_cut(const Kv8AttArgs& a, const SeqRows& r) {
     SeqCut s;
-    s.start = sr.start;
-    s.count = min(sr.count, a.max_new);
-    s.pos0 = a.pos0[b];
-    s.n_pos = (int)min(max(s.pos0 + s.count, (int64_t)0), (int64_t)a.c.max_pos);
+    s.count = min(r.count, a.max_new);
+    s.n_pos = (int)min(max((int64_t)r.pos0 + s.count, (int64_t)0), (int64_t)a.c.max_pos);
     s.tiles = (uint32_t)(s.count * a.rep + ROWS - 1) / ROWS;
     s.spans = s.count ? (uint32_t)max((s.n_pos + kAttSpan - 1) / kAttSpan, 1) : 0u;
     return s;
 }
-// spans of a stretch
+
+// Spans of a stretch, the same for all sequences.  With few row tiles: as few spans as let all stretches run side by side (64 rows against
+// 500 to 4000 positions, four sequences: 24 us with 512 stretches for 512 places, 26 with 448, 32 with 320 and with 832).  With more, twice
+// as many stretches as places: sequences differ in length, and short stretches fill the gaps (59 sequences of 14 to 16000 positions: 114 us
+// with a stretch a place, 104 with two, 106 with four).  A sequence of more than 128 spans is not cut into single ones, as what they
+// leave has to be joined (30000 positions: 17.6 us cut into single spans, 14.8 into pairs).
 template <int ROWS>
-__device__ __forceinline__ uint32_t stretch_of(const Kv8AttArgs& a) {
-    const uint64_t all = total_units(a.n_seq, [&](int b) {
-        const SeqCut s = seq_cut<ROWS>(a, b);
+__device__ __forceinline__ uint32_t stretch_of(const Kv8AttArgs& a, const Sequences& seqs) {
+    const uint64_t all = seqs.total([&](const SeqRows& r) {
+        const SeqCut s = seq_cut<ROWS>(a, r);
         return s.tiles * s.spans;
     });
-    return max((uint32_t)((all + (uint32_t)a.want - 1) / (uint32_t)a.want), 1u);
+    const uint32_t tiles = (uint32_t)seqs.total([&](const SeqRows& r) { return seq_cut<ROWS>(a, r).tiles; });
+    const uint32_t places = (uint32_t)a.places;
+    auto share = [&](uint32_t n) { return (uint32_t)((all + n - 1) / n); };
+    if (2 * tiles > places) return max(share(2 * places), 1u);
+    uint32_t stretch = max(share(places), all > 128 * (uint64_t)tiles ? 2u : 1u);
+    const uint32_t enough = share(places - tiles);  // a sequence's last stretch may be short: no more than one for each row tile
+    while (stretch < enough && seqs.total([&](const SeqRows& r) {
+               const SeqCut s = seq_cut<ROWS>(a, r);
+               return s.tiles * ((s.spans + stretch - 1) / stretch);
+           }) > places)
+        stretch = min(stretch + max(stretch / 16, 1u), enough);
+    return stretch;
 }
 
 typedef int i32x2 __attribute__((ext_vector_type(2)));
@@ -257,14 +271,32 @@ __device__ __forceinline__ bf16x8 e4m3x8_to_bf16(uint32_t c0, uint32_t c1, float
     return f.v;
 }
 
-// place of 16-byte piece c of row r in a tile of values: eight rows of a transposing read side by side fall into different banks
+// Byte offset of 16-byte piece c of row r in a tile of keys or values: the pieces of a row are turned by its number, which spreads the
+// reads over the banks -- keys: sixteen rows side by side, values: eight rows of a transposing read, sixteen lanes each.
 template <int D>
-__device__ __forceinline__ int value_place(int r, int c) {
-    constexpr int kPieces = D / 16;
-    const int turn = D == 64 ? (r >> 2) & 3 : D == 128 ? (r >> 1) & 7 : r & 15;
-    return 16 * (r * kPieces + (c ^ turn));
+__device__ __forceinline__ int turned(int r, int c) {
+    return c ^ (D == 64 ? (r >> 2) & 3 : D == 128 ? (r >> 1) & 7 : r & 15);
+}
+template <int D>
+__device__ __forceinline__ int tile_place(int r, int c) {
+    return 16 * (r * (D / 16) + turned<D>(r, c));
 }
 
+// Eight positions of one dimension in every lane, for 16 N dimensions: sixteen lanes read eight rows of sixteen dimensions.  The wait
+// is inside, as the compiler would wait for the tile under way as well: it cannot tell the two buffers apart.
+template <int N>
+__device__ __forceinline__ void read_values(i32x2 (&v)[N], const uint32_t (&at)[N]) {
+    static_assert(N % 4 == 0, "read four at a time");
+#pragma unroll
+    for (int i = 0; i < N; i += 4)
+        asm volatile(
+            "ds_read_b64_tr_b8 %0, %4\n\tds_read_b64_tr_b8 %1, %5\n\tds_read_b64_tr_b8 %2, %6\n\tds_read_b64_tr_b8 %3, %7\n\ts_waitcnt lgkmcnt(0)"
+            : "=&v"(v[i]), "=&v"(v[i + 1]), "=&v"(v[i + 2]), "=&v"(v[i + 3])
+            : "v"(at[i]), "v"(at[i + 1]), "v"(at[i + 2]), "v"(at[i + 3])
+            : "memory");
+}
+
+constexpr int kv8_lds(int dim) { return kAttWaves * 2 * 2 * 32 * dim; }
 // wavefronts that share a SIMD's registers
 constexpr int kv8_waves(int dim, int nr) { return dim == 256 ? 1 : dim * nr <= 64 ? 4 : dim * nr <= 128 ? 3 : 2; }
 
@@ -272,65 +304,72 @@ template <int D, int NR>
 __global__ __launch_bounds__(64 * kAttWaves, kv8_waves(D, NR)) void kv8_attention_kernel(Kv8AttArgs a) {
     constexpr int kRows = 16 * NR, kDb = D / 16, kJ = D / 64, kPieces = D / 16, kTile = 32 * D, kLoads = kTile / 1024;
     constexpr int kORow = D + 4;  // floats
-    constexpr int kMerge = kAttWaves * (16 * kORow + 32) * 4, kLds = kAttWaves * kTile > kMerge ? kAttWaves * kTile : kMerge;
-    __shared__ __attribute__((aligned(16))) uint8_t smem[kLds];
+    static_assert(kAttWaves * (16 * kORow + 32) * 4 <= kv8_lds(D), "the wavefronts' results fit where the tiles were");
+    extern __shared__ __attribute__((aligned(16))) uint8_t smem[];  // [wave][buffer][keys, values][32][D]
     const int tid = threadIdx.x, lane = tid & 63, wave = __builtin_amdgcn_readfirstlane(tid >> 6), n = lane & 15, g = lane >> 4;
     const int grp = blockIdx.x % a.c.n_kv;
     const uint32_t unit = blockIdx.x / a.c.n_kv;
-    const uint32_t stretch = stretch_of<kRows>(a);
-    const SeqUnit u = find_unit(unit, a.n_seq, [&](int b) {
-        const SeqCut s = seq_cut<kRows>(a, b);
+    const Sequences seqs(a.row_start, a.pos0, a.n_seq, a.n_rows);
+    const uint32_t stretch = stretch_of<kRows>(a, seqs);
+    const SeqUnit u = seqs.find(unit, [&](const SeqRows& r) {
+        const SeqCut s = seq_cut<kRows>(a, r);
         return s.tiles * ((s.spans + stretch - 1) / stretch);
     });
     if (u.seq < 0) return;
-    const SeqCut sc = seq_cut<kRows>(a, u.seq);
+    const SeqCut sc = seq_cut<kRows>(a, u.rows);
+    const int64_t pos0 = u.rows.pos0;
     const uint32_t cuts = (sc.spans + stretch - 1) / stretch;
     const int tile = (int)(u.index / cuts), cut = (int)(u.index % cuts);
     const int D_used = a.c.head_dim, rep = a.rep, n_used = sc.count * rep;  // rows of the sequence
     const int first = kRows * tile;
     // positions of this workgroup, up to the last that its last row attends to
-    const int reach_last = (int)min(sc.pos0 + (min(first + kRows, n_used) - 1) / rep, (int64_t)a.c.max_pos - 1);
+    const int reach_last = (int)min(pos0 + (min(first + kRows, n_used) - 1) / rep, (int64_t)a.c.max_pos - 1);
     const int from = cut * (int)stretch * kAttSpan, to = min(from + (int)stretch * kAttSpan, reach_last + 1);
-    const int reach_first = (int)min(max(sc.pos0 + first / rep, (int64_t)-1), (int64_t)a.c.max_pos);  // of the tile's first row
+    const int reach_first = (int)min(max(pos0 + first / rep, (int64_t)-1), (int64_t)a.c.max_pos);  // of the tile's first row
+    const int rows_here = min(n_used - first, kRows);  // row tiles past these are left out
     const size_t head = (size_t)u.seq * a.c.n_kv + grp;
     const uint8_t* kg = a.c.k + head * a.c.max_pos * D_used;
     const uint8_t* vg = a.c.v + head * a.c.max_pos * D_used;
     const float* ks = a.c.k_scale + head * (a.c.max_pos / kBlock);
     const float* vs = a.c.v_scale + head * (a.c.max_pos / kBlock);
-    uint8_t* vt = smem + wave * kTile;
+    uint8_t* ring = smem + wave * 4 * kTile;
 
-    u32x4 kr[2][kJ], vr[kLoads];
-    float kscale = 0.f, vscale = 0.f;
-    // K: lane (n, g) brings dimensions 64 j + 16 g .. + 15 of position 8 (n / 4) + 4 b + n % 4; V: pieces in memory's order
-    auto request = [&](int base) __attribute__((always_inline)) {
-#pragma unroll
-        for (int b = 0; b < 2; ++b)
-#pragma unroll
-            for (int jj = 0; jj < kJ; ++jj) {
-                const int d = 64 * jj + 16 * g;
-                kr[b][jj] = u32x4{0, 0, 0, 0};
-                if (d < D_used)
-                    kr[b][jj] = *reinterpret_cast<const u32x4*>(kg + (size_t)(base + 8 * (n >> 2) + 4 * b + (n & 3)) * D_used + d);
+    if (D_used < D) {  // dimensions that the heads do not have: zero, and never written again
+        for (int i = lane; i < 4 * kTile / 16; i += 64) reinterpret_cast<u32x4*>(ring)[i] = u32x4{0, 0, 0, 0};
+        __builtin_amdgcn_s_waitcnt(0xC07F);  // lgkmcnt(0): in front of what follows
+        asm volatile("" ::: "memory");
+    }
+    // A tile straight into LDS: 2 kLoads requests of 1 KiB, rows lane / kPieces + 64 / kPieces i.
+    const int r0 = lane / kPieces, c0 = lane % kPieces;
+    auto request = [&](int base, int buf) __attribute__((always_inline)) {
+        const uint8_t* kb = kg + (size_t)base * D_used;
+        const uint8_t* vb = vg + (size_t)base * D_used;
+        auto* to_lds = (__attribute__((address_space(3))) uint8_t*)(ring + 2 * buf * kTile);
+        auto piece = [&](int i) __attribute__((always_inline)) {
+            const int r = r0 + 64 / kPieces * i, d = 16 * turned<D>(r, c0);
+            if (D_used == D || d < D_used) {
+                __builtin_amdgcn_global_load_lds((const __attribute__((address_space(1))) void*)(kb + (uint32_t)(r * D_used + d)), to_lds + 1024 * i, 16, 0, 0);
+                __builtin_amdgcn_global_load_lds((const __attribute__((address_space(1))) void*)(vb + (uint32_t)(r * D_used + d)), to_lds + kTile + 1024 * i, 16, 0, 0);
             }
+        };
+        if (D_used == D) {
 #pragma unroll
-        for (int i = 0; i < kLoads; ++i) {
-            const int piece = 64 * i + lane, r = piece / kPieces, d = 16 * (piece % kPieces);
-            vr[i] = u32x4{0, 0, 0, 0};
-            if (d < D_used) vr[i] = *reinterpret_cast<const u32x4*>(vg + (size_t)(base + r) * D_used + d);
+            for (int i = 0; i < kLoads; ++i) piece(i);
+        } else {
+#pragma unroll
+            for (int i = 0; i < kLoads; ++i) piece(i);
         }
-        kscale = ks[base / kBlock];
-        vscale = vs[base / kBlock];
     };
     int base = from + 32 * wave;
-    if (base < to) request(base);
+    if (base < to) request(base, 0);
 
     bf16x8 q[NR][2 * kJ];  // in the order of the keys' dimensions
     int reach[NR];         // last position of row n
 #pragma unroll
     for (int t = 0; t < NR; ++t) {
         const int row = min(first + 16 * t + n, n_used - 1), token = row / rep, r = row - token * rep;
-        reach[t] = (int)min(max(sc.pos0 + token, (int64_t)-1), (int64_t)a.c.max_pos - 1);
-        const uint16_t* src = a.q + (size_t)(sc.start + token) * a.q_stride + (size_t)(grp * rep + r) * D_used;
+        reach[t] = (int)min(max(pos0 + token, (int64_t)-1), (int64_t)a.c.max_pos - 1);
+        const uint16_t* src = a.q + (size_t)(u.rows.start + token) * a.q_stride + (size_t)(grp * rep + r) * D_used;
 #pragma unroll
         for (int jj = 0; jj < kJ; ++jj) {
             const int d = 64 * jj + 16 * g;
@@ -353,15 +392,48 @@ __global__ __launch_bounds__(64 * kAttWaves, kv8_waves(D, NR)) void kv8_attentio
 #pragma unroll
         for (int d = 0; d < kDb; ++d) o[t][d] = f32x4{0.f, 0.f, 0.f, 0.f};
     }
-    for (; base < to; base += kAttSpan) {
+    const int key_row = 8 * (n >> 2) + (n & 3);
+    uint32_t value_at[kDb];
+#pragma unroll
+    for (int d = 0; d < kDb; ++d)
+        value_at[d] = (uint32_t)(uintptr_t)(const __attribute__((address_space(3))) uint8_t*)ring + kTile + tile_place<D>(8 * g + (n >> 1), d) + 8 * (n & 1);
+    // Waits for vector memory are written out: one that the compiler puts where a value is used would be one for the requests as well.
+    float k_scales = 0.f, v_scales = 0.f;  // of the wavefront's next 64 tiles, one in each lane
+    auto load_scales = [&]() __attribute__((always_inline)) {
+        const int block = min(base / kBlock + kAttWaves * lane, a.c.max_pos / kBlock - 1);
+        k_scales = ks[block];
+        v_scales = vs[block];
+    };
+    if (base < to) load_scales();
+    __builtin_amdgcn_s_waitcnt(0x0F70);  // the scales, the queries and the first tile
+    asm volatile("" : "+v"(k_scales), "+v"(v_scales)::"memory");
+    for (int buf = 0, i = 0; base < to; base += kAttSpan, buf ^= 1, ++i) {
+        if (i && (i & 63) == 0) {
+            load_scales();
+            __builtin_amdgcn_s_waitcnt(0x0F70);
+            asm volatile("" : "+v"(k_scales), "+v"(v_scales)::"memory");
+        }
+        const float c = __int_as_float(__builtin_amdgcn_readlane(__float_as_int(k_scales), i & 63)) * a.scale;
+        const float v_scale = __int_as_float(__builtin_amdgcn_readlane(__float_as_int(v_scales), i & 63));
+        if (base + kAttSpan < to) {
+            request(base + kAttSpan, buf ^ 1);
+            asm volatile("" ::: "memory");
+            __builtin_amdgcn_s_waitcnt(0x0F70 | ((2 * kLoads) & 15) | ((2 * kLoads) >> 4 << 14));  // all but the requests just made
+        } else {
+            __builtin_amdgcn_s_waitcnt(0x0F70);
+        }
+        asm volatile("" ::: "memory");
+        const uint8_t* kt = ring + 2 * buf * kTile;
         f32x4 s[NR][2];
 #pragma unroll
         for (int b = 0; b < 2; ++b) {
+            // lane (n, g): dimensions 64 j + 16 g .. + 15 of position 8 (n / 4) + 4 b + n % 4
             bf16x8 kf[2 * kJ];
 #pragma unroll
             for (int jj = 0; jj < kJ; ++jj) {
-                kf[2 * jj] = e4m3x8_to_bf16(kr[b][jj][0], kr[b][jj][1], 1.0f);
-                kf[2 * jj + 1] = e4m3x8_to_bf16(kr[b][jj][2], kr[b][jj][3], 1.0f);
+                const u32x4 x = *reinterpret_cast<const u32x4*>(kt + tile_place<D>(key_row + 4 * b, 4 * jj + g));
+                kf[2 * jj] = e4m3x8_to_bf16(x[0], x[1], 1.0f);
+                kf[2 * jj + 1] = e4m3x8_to_bf16(x[2], x[3], 1.0f);
             }
 #pragma unroll
             for (int t = 0; t < NR; ++t) {
@@ -370,28 +442,14 @@ __global__ __launch_bounds__(64 * kAttWaves, kv8_waves(D, NR)) void kv8_attentio
                 for (int jj = 0; jj < 2 * kJ; ++jj) s[t][b] = __builtin_amdgcn_mfma_f32_16x16x32_bf16(kf[jj], q[t][jj], s[t][b], 0, 0, 0);
             }
         }
-        const float c = kscale * a.scale, v_scale = vscale;
         const bool masked = base + 31 > reach_first;
-        bool odd_values = false;  // a value of a position that not every row attends to is NaN
-        if (masked) {
-            const int n_here = to - base;  // positions past the last are whatever the memory held
-#pragma unroll
-            for (int i = 0; i < kLoads; ++i) {
-                if ((64 * i + lane) / kPieces >= n_here) vr[i] = u32x4{0, 0, 0, 0};
-#pragma unroll
-                for (int e = 0; e < 4; ++e) odd_values |= ((((vr[i][e] & 0x7f7f7f7fu) + 0x01010101u) & 0x80808080u) != 0);
-            }
-            odd_values = __any(odd_values);
-        }
-#pragma unroll
-        for (int i = 0; i < kLoads; ++i) {
-            const int piece = 64 * i + lane;
-            *reinterpret_cast<u32x4*>(vt + value_place<D>(piece / kPieces, piece % kPieces)) = vr[i];
-        }
-        if (base + kAttSpan < to) request(base + kAttSpan);
         bf16x8 p[NR];
 #pragma unroll
         for (int t = 0; t < NR; ++t) {
+            Frag zero;
+            zero.q = u32x4{0, 0, 0, 0};
+            p[t] = zero.v;
+            if (t && 16 * t >= rows_here) continue;
             float w[8], mx = -3.0e38f;
 #pragma unroll
             for (int e = 0; e < 8; ++e) {
@@ -417,24 +475,31 @@ __global__ __launch_bounds__(64 * kAttWaves, kv8_waves(D, NR)) void kv8_attentio
             for (int e = 0; e < 4; ++e) pair.u[e] = pack_bf16(w[2 * e], w[2 * e + 1]);
             p[t] = pair.v;
         }
-        asm volatile("" ::: "memory");
-        __builtin_amdgcn_wave_barrier();
-        // sixteen lanes read eight rows of sixteen dimensions; each gets eight positions of its own dimension
-        auto values = [&](int d) __attribute__((always_inline)) {
-            const auto* src = (const __attribute__((address_space(3))) uint8_t*)vt + value_place<D>(8 * g + (n >> 1), d) + 8 * (n & 1);
-            return __builtin_amdgcn_ds_read_tr8_b64_v2i32((__attribute__((address_space(3))) i32x2*)src);
-        };
-        if (!odd_values) {
+        i32x2 codes[kDb];
+        {
+            uint32_t at[kDb];
+#pragma unroll
+            for (int d = 0; d < kDb; ++d) at[d] = value_at[d] + 2 * buf * kTile;
+            read_values(codes, at);
+        }
+        bool odd = false;  // a value of a position that not every row attends to is NaN
+        if (masked) {
+            uint32_t nan = 0;
+#pragma unroll
+            for (int d = 0; d < kDb; ++d) nan |= (((uint32_t)codes[d][0] & 0x7f7f7f7fu) + 0x01010101u) | (((uint32_t)codes[d][1] & 0x7f7f7f7fu) + 0x01010101u);
+            odd = __any((nan & 0x80808080u) != 0);
+        }
+        if (!odd) {
 #pragma unroll
             for (int d = 0; d < kDb; ++d) {
-                const i32x2 codes = values(d);
-                const bf16x8 v = e4m3x8_to_bf16((uint32_t)codes[0], (uint32_t)codes[1], v_scale);
+                const bf16x8 v = e4m3x8_to_bf16((uint32_t)codes[d][0], (uint32_t)codes[d][1], v_scale);
 #pragma unroll
                 for (int t = 0; t < NR; ++t) o[t][d] = __builtin_amdgcn_mfma_f32_16x16x32_bf16(v, p[t], o[t][d], 0, 0, 0);
             }
         } else {
-            // A weight of zero times NaN is NaN, also where the row does not attend to the position: NaN goes in as zero, and where a row
-            // attends to one -- a product of two masks of ones tells -- its result becomes NaN.
+            // A weight of zero times NaN is NaN, also where the row does not attend to the position -- a later token's, or one that nothing
+            // has been stored in: NaN goes in as zero, and where a row attends to one -- a product of two masks of ones tells -- its result
+            // becomes NaN.
             bf16x8 attends[NR];
 #pragma unroll
             for (int t = 0; t < NR; ++t) {
@@ -446,8 +511,7 @@ __global__ __launch_bounds__(64 * kAttWaves, kv8_waves(D, NR)) void kv8_attentio
             }
 #pragma unroll
             for (int d = 0; d < kDb; ++d) {
-                const i32x2 codes = values(d);
-                const uint32_t c0 = (uint32_t)codes[0], c1 = (uint32_t)codes[1];
+                const uint32_t c0 = (uint32_t)codes[d][0], c1 = (uint32_t)codes[d][1];
                 const uint32_t n0 = (((c0 & 0x7f7f7f7fu) + 0x01010101u) >> 7) & 0x01010101u, n1 = (((c1 & 0x7f7f7f7fu) + 0x01010101u) >> 7) & 0x01010101u;
                 const bf16x8 v = e4m3x8_to_bf16(c0 & ~(n0 * 0xffu), c1 & ~(n1 * 0xffu), v_scale);
                 const bf16x8 nan = e4m3x8_to_bf16(n0 * 0x38u, n1 * 0x38u, 1.0f);
@@ -460,8 +524,6 @@ __global__ __launch_bounds__(64 * kAttWaves, kv8_waves(D, NR)) void kv8_attentio
                 }
             }
         }
-        asm volatile("" ::: "memory");
-        __builtin_amdgcn_wave_barrier();  // the next tile overwrites the values
     }
 
     // the wavefronts' results meet in LDS, sixteen rows at a time
@@ -469,6 +531,7 @@ __global__ __launch_bounds__(64 * kAttWaves, kv8_waves(D, NR)) void kv8_attentio
     float2* mstat = reinterpret_cast<float2*>(mo + kAttWaves * 16 * kORow);  // [wave][16]
 #pragma unroll
     for (int t = 0; t < NR; ++t) {
+        if (t && 16 * t >= rows_here) break;
         const float sum = sum_quarters(sum_halves(l[t]));
         __syncthreads();
 #pragma unroll
@@ -488,9 +551,12 @@ __global__ __launch_bounds__(64 * kAttWaves, kv8_waves(D, NR)) void kv8_attentio
             }
             const int token = row / rep;
             // a row that attends to nothing is zero
-            const float inv = sc.pos0 + token < 0 ? 0.f : 1.0f / all;
+            const float inv = pos0 + token < 0 ? 0.f : 1.0f / all;
             const size_t slot = ((size_t)unit * a.c.n_kv + grp) * kRows + 16 * t + r16;
-            if (cuts > 1 && (tid & 15) == 0) a.stat[slot] = make_float2(top, all);
+            if ((tid & 15) == 0) {
+                if (cuts > 1) a.stat[slot] = make_float2(top, all);
+                if (cut == 0) a.join[((size_t)u.seq * a.max_new + token) * (a.c.n_kv * rep) + grp * rep + (row - token * rep)] = make_uint2(unit, cuts);
+            }
 #pragma unroll
             for (int d = 4 * (tid & 15); d < D; d += 64) {
                 if (d >= D_used) break;
@@ -501,7 +567,7 @@ __global__ __launch_bounds__(64 * kAttWaves, kv8_waves(D, NR)) void kv8_attentio
                     *reinterpret_cast<f32x4*>(a.part + slot * D + d) = x;
                 } else {
                     x *= inv;
-                    uint16_t* dst = a.out + ((size_t)(sc.start + token) * a.c.n_kv * rep + (size_t)grp * rep + (row - token * rep)) * D_used + d;
+                    uint16_t* dst = a.out + ((size_t)(u.rows.start + token) * a.c.n_kv * rep + (size_t)grp * rep + (row - token * rep)) * D_used + d;
                     *reinterpret_cast<uint2*>(dst) = make_uint2(pack_bf16(x[0], x[1]), pack_bf16(x[2], x[3]));
                 }
             }
@@ -509,51 +575,91 @@ __global__ __launch_bounds__(64 * kAttWaves, kv8_waves(D, NR)) void kv8_attentio
     }
 }
 
-// Joins the stretches of a sequence that was cut: a wavefront for each (row, query head), a lane for D / 64 dimensions.
-template <int D, int NR>
+// Joins the stretches of the rows that were cut: W wavefronts for each (row, query head), D / 4 lanes a stretch.
+template <int D, int NR, int W>
 __global__ __launch_bounds__(256) void kv8_combine_kernel(Kv8AttArgs a) {
-    constexpr int kRows = 16 * NR, kPer = D / 64;
-    const int lane = threadIdx.x & 63, n_heads = a.c.n_kv * a.rep;
-    const uint32_t item = blockIdx.x * 4 + (uint32_t)__builtin_amdgcn_readfirstlane((int)threadIdx.x >> 6);
-    const int row = (int)(item / (uint32_t)n_heads), h = (int)(item % (uint32_t)n_heads);
-    if (row >= a.n_rows) return;
-    const SeqUnit by_row = find_unit((uint32_t)row, a.n_seq, [&](int b) { return (uint32_t)seq_rows(a.row_start, b, a.n_rows).count; });
-    if (by_row.seq < 0) return;
-    const SeqCut sc = seq_cut<kRows>(a, by_row.seq);
-    const int token = row - sc.start;
-    if (token < 0 || token >= sc.count) return;
-    const uint32_t stretch = stretch_of<kRows>(a), cuts = (sc.spans + stretch - 1) / stretch;
-    if (cuts <= 1) return;
-    const uint32_t before = (uint32_t)total_units(by_row.seq, [&](int b) {
-        const SeqCut s = seq_cut<kRows>(a, b);
-        return s.tiles * ((s.spans + stretch - 1) / stretch);
-    });
-    const int grp = h / a.rep, local = token * a.rep + (h - grp * a.rep), tile = local / kRows;
-    const uint32_t unit0 = before + (uint32_t)tile * cuts;
-    if (unit0 + cuts > a.bound) return;
-    const size_t slot0 = ((size_t)unit0 * a.c.n_kv + grp) * kRows + local % kRows, step = (size_t)a.c.n_kv * kRows;
-    float top = -3.0e38f;
-    for (uint32_t i = lane; i < cuts; i += 64) top = fmaxf(top, a.stat[slot0 + i * step].x);
-    top = max_quarters(max_halves(top));
+    constexpr int kRows = 16 * NR, kLanes = D / 4, kSide = 64 * W / kLanes;  // stretches side by side
+    __shared__ __attribute__((aligned(16))) float sums[W > 1 ? kSide : 1][W > 1 ? D : 1];
+    __shared__ float2 stats[W > 1 ? kSide : 1];
+    const int n_heads = a.c.n_kv * a.rep, tid = threadIdx.x & (64 * W - 1);
+    const uint32_t item = blockIdx.x * (4 / W) + (W > 1 ? 0u : (uint32_t)__builtin_amdgcn_readfirstlane((int)threadIdx.x >> 6));
+    const uint32_t h = item % (uint32_t)n_heads, row = item / (uint32_t)n_heads;  // row: sequence times max_new + token
+    if (row >= (uint32_t)a.n_seq * (uint32_t)a.max_new) return;
+    const uint2 join = a.join[(size_t)row * n_heads + h];
+    const int seq = (int)(row / (uint32_t)a.max_new), token = (int)(row % (uint32_t)a.max_new);
+    const SeqRows sr = seq_rows(a.row_start, a.pos0, seq, a.n_rows);
+    if (token >= sr.count) return;  // nobody wrote the entry
+    const uint32_t cuts = (uint32_t)__builtin_amdgcn_readfirstlane((int)join.y), unit0 = (uint32_t)__builtin_amdgcn_readfirstlane((int)join.x);
+    if (cuts <= 1 || unit0 >= a.bound || cuts > a.bound - unit0) return;
+    const int grp = (int)h / a.rep, local = (token * a.rep + ((int)h - grp * a.rep)) % kRows;
+    const size_t slot0 = ((size_t)unit0 * a.c.n_kv + grp) * kRows + local, step = (size_t)a.c.n_kv * kRows;
+    const int side = tid / kLanes, d = 4 * (tid % kLanes);
+    const bool used = d < a.c.head_dim;
+    float top = -3.0e38f, all = 0.f;
+    f32x4 x = f32x4{0.f, 0.f, 0.f, 0.f};
+    // a running maximum over eight stretches at a time, so that eight loads are under way
+    for (uint32_t i = side; i < cuts; i += 8 * kSide) {
+        float2 st[8];
+        f32x4 v[8];
+        float most = top;
 #pragma unroll
-    for (int i = 1; i < 16; i <<= 1) top = fmaxf(top, __shfl_xor(top, i));
-    float all = 0.f, x[kPer];
+        for (int e = 0; e < 8; ++e) {
+            const uint32_t at = i + e * kSide;
+            st[e] = make_float2(-3.0e38f, 0.f);
+            v[e] = f32x4{0.f, 0.f, 0.f, 0.f};
+            if (at < cuts) {
+                st[e] = a.stat[slot0 + at * step];
+                if (used) v[e] = *reinterpret_cast<const f32x4*>(a.part + (slot0 + at * step) * D + d);
+            }
+        }
 #pragma unroll
-    for (int i = 0; i < kPer; ++i) x[i] = 0.f;
-#pragma unroll 4
-    for (uint32_t i = 0; i < cuts; ++i) {
-        const float2 st = a.stat[slot0 + i * step];
-        const float w = __builtin_amdgcn_exp2f(st.x - top);
-        all += w * st.y;
-        const float* src = a.part + (slot0 + i * step) * D + kPer * lane;
+        for (int e = 0; e < 8; ++e) most = fmaxf(most, st[e].x);
+        const float f = __builtin_amdgcn_exp2f(top - most);
+        top = most;
+        all *= f;
+        x *= f;
 #pragma unroll
-        for (int e = 0; e < kPer; ++e) x[e] += w * (kPer * lane + e < a.c.head_dim ? src[e] : 0.f);
+        for (int e = 0; e < 8; ++e) {
+            const float w = __builtin_amdgcn_exp2f(st[e].x - top);
+            all += w * st[e].y;
+            x += v[e] * w;
+        }
     }
-    const float inv = sc.pos0 + token < 0 ? 0.f : 1.0f / all;
-    uint16_t* dst = a.out + ((size_t)row * n_heads + h) * a.c.head_dim + kPer * lane;
+    if constexpr (W > 1) {
+        *reinterpret_cast<f32x4*>(&sums[side][d]) = x;
+        if (d == 0) stats[side] = make_float2(top, all);
+        __syncthreads();
+        if (side) return;
+        const float own = top;
 #pragma unroll
-    for (int e = 0; e < kPer; ++e)
-        if (kPer * lane + e < a.c.head_dim) dst[e] = f32_to_bf16(x[e] * inv);
+        for (int e = 1; e < kSide; ++e) top = fmaxf(top, stats[e].x);
+        const float f = __builtin_amdgcn_exp2f(own - top);
+        all *= f;
+        x *= f;
+#pragma unroll
+        for (int e = 1; e < kSide; ++e) {
+            const float w = __builtin_amdgcn_exp2f(stats[e].x - top);
+            all += w * stats[e].y;
+            x += *reinterpret_cast<const f32x4*>(&sums[e][d]) * w;
+        }
+    } else {
+#pragma unroll
+        for (int o = kLanes; o < 64; o <<= 1) {
+            const float other = __shfl_xor(top, o), most = fmaxf(top, other), f = __builtin_amdgcn_exp2f(top - most);
+            all *= f;
+            all += __shfl_xor(all, o);
+            x *= f;
+#pragma unroll
+            for (int e = 0; e < 4; ++e) x[e] += __shfl_xor(x[e], o);
+            top = most;
+        }
+        if (side) return;
+    }
+    if (!used) return;
+    // a row that attends to nothing is zero
+    x *= (int64_t)sr.pos0 + token < 0 ? 0.f : 1.0f / all;
+    *reinterpret_cast<uint2*>(a.out + ((size_t)(sr.start + token) * n_heads + h) * a.c.head_dim + d) =
+        make_uint2(pack_bf16(x[0], x[1]), pack_bf16(x[2], x[3]));
 }
 
 // Rows of a workgroup: as many of a sequence's as there can be, up to what the registers hold.
@@ -563,13 +669,14 @@ Kv8Plan kv8_plan(int n_heads, int n_kv, int head_dim, int n_seq, int max_new) {
     p.dim = head_dim <= 64 ? 64 : head_dim <= 128 ? 128 : 256;
     p.nr = rows <= 16 || p.dim == 256 ? 1 : rows <= 32 || p.dim == 128 ? 2 : 4;
     const int kv = n_kv;
-    p.want = (2 * device_cu_count() + kv - 1) / kv;
+    p.places = (2 * device_cu_count() + kv - 1) / kv;
     p.tiles = (rows + 16 * p.nr - 1) / (16 * p.nr);
     // units: sum of tiles * ceil(spans / stretch) <= sum of tiles * spans / stretch + sum of tiles
-    p.bound = (uint32_t)p.want + (uint32_t)n_seq * (uint32_t)p.tiles;
+    p.bound = 2 * (uint32_t)p.places + (uint32_t)n_seq * (uint32_t)p.tiles;
     const size_t slots = (size_t)p.bound * kv * 16 * p.nr;
     p.stat_off = slots * p.dim * sizeof(float);
-    p.bytes = p.stat_off + slots * sizeof(float2);
+    p.join_off = p.stat_off + slots * sizeof(float2);
+    p.bytes = p.join_off + (size_t)n_seq * max_new * n_heads * sizeof(uint2);
     return p;
 }
 
@@ -579,17 +686,32 @@ hipError_t launch_kv8_attention(const Kv8Args& c, const uint16_t* q, int64_t q_s
     if (n_rows == 0 || n_seq == 0) return hipSuccess;
     const Kv8Plan p = kv8_plan(n_heads, c.n_kv, c.head_dim, n_seq, max_new);
     const int rep = n_heads / c.n_kv;
-    Kv8AttArgs a = {c, q, q_stride, row_start, pos0, n_seq, n_rows, max_new, rep, p.want, p.bound,
+    Kv8AttArgs a = {c, q, q_stride, row_start, pos0, n_seq, n_rows, max_new, rep, p.places, p.bound,
                     (float)(1.4426950408889634 / sqrt((double)c.head_dim)), out, static_cast<float*>(ws),
-                    reinterpret_cast<float2*>(static_cast<uint8_t*>(ws) + p.stat_off)};
+                    reinterpret_cast<float2*>(static_cast<uint8_t*>(ws) + p.stat_off),
+                    reinterpret_cast<uint2*>(static_cast<uint8_t*>(ws) + p.join_off)};
+    if (kv8_lds(p.dim) > 65536) {
+        static std::atomic<bool> raised{false};  // once, at the first call (a warm-up call precedes any graph capture)
+        if (!raised.load(std::memory_order_acquire)) {
+            const hipError_t e = hipFuncSetAttribute(reinterpret_cast<const void*>(&kv8_attention_kernel<256, 1>),
+                                                     hipFuncAttributeMaxDynamicSharedMemorySize, kv8_lds(256));
+            if (e != hipSuccess) return e;
+            raised.store(true, std::memory_order_release);
+        }
+    }
     // row tiles that these rows can have
     const uint64_t tiles = (uint64_t)n_rows * rep / (16 * p.nr) + (uint64_t)(n_seq < n_rows ? n_seq : n_rows);
     const uint64_t most = (uint64_t)n_seq * p.tiles;
-    const dim3 grid((unsigned)((p.want + (tiles < most ? tiles : most)) * c.n_kv)), join((unsigned)(((uint64_t)n_rows * n_heads + 3) / 4));
-#define SD2_KV8(DIM, R)                                                                              \
-    if (p.dim == DIM && p.nr == R) {                                                                 \
-        hipLaunchKernelGGL((kv8_attention_kernel<DIM, R>), grid, dim3(64 * kAttWaves), 0, s, a);      \
-        if (c.max_pos > kAttSpan) hipLaunchKernelGGL((kv8_combine_kernel<DIM, R>), join, dim3(256), 0, s, a); \
+    const dim3 grid((unsigned)((2 * p.places + (tiles < most ? tiles : most)) * c.n_kv));
+    // (row, query head) pairs; few of them have many stretches each: four wavefronts
+    const uint64_t pairs = (uint64_t)n_seq * max_new * n_heads;
+    const bool wide = pairs <= 8u * (unsigned)device_cu_count();
+    const dim3 join((unsigned)(wide ? pairs : (pairs + 3) / 4));
+#define SD2_KV8(DIM, R)                                                                                                   \
+    if (p.dim == DIM && p.nr == R) {                                                                                      \
+        hipLaunchKernelGGL((kv8_attention_kernel<DIM, R>), grid, dim3(64 * kAttWaves), kv8_lds(DIM), s, a);               \
+        if (c.max_pos > kAttSpan && wide) hipLaunchKernelGGL((kv8_combine_kernel<DIM, R, 4>), join, dim3(256), 0, s, a);  \
+        if (c.max_pos > kAttSpan && !wide) hipLaunchKernelGGL((kv8_combine_kernel<DIM, R, 1>), join, dim3(256), 0, s, a); \
     }
     SD2_KV8(64, 1) SD2_KV8(64, 2) SD2_KV8(64, 4)
     SD2_KV8(128, 1) SD2_KV8(128, 2)

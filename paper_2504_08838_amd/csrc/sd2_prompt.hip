@@ -47,13 +47,13 @@ __global__ __launch_bounds__(64 * kPromptWaves, D == 256 ? 1 : 2) void prompt_at
     __shared__ __attribute__((aligned(16))) uint8_t smem[2][2][kBytes];  // [buffer][keys, values]
     const int tid = threadIdx.x, lane = tid & 63, wave = __builtin_amdgcn_readfirstlane(tid >> 6), n = lane & 31, h = lane >> 5;
     const int grp = blockIdx.x % a.n_kv, rep = a.rep, hd = a.head_dim;
-    auto tiles_of = [&](int b) { return (uint32_t)(((int64_t)seq_rows(a.row_start, b, a.n_rows).count * rep + kPromptRows - 1) / kPromptRows); };
-    const SeqUnit u = find_unit(blockIdx.x / a.n_kv, a.n_seq, tiles_of);
+    auto tiles_of = [&](const SeqRows& r) { return (uint32_t)(r.count * rep + kPromptRows - 1) / kPromptRows; };
+    const SeqUnit u = Sequences(a.row_start, nullptr, a.n_seq, a.n_rows).find(blockIdx.x / a.n_kv, tiles_of);
     if (u.seq < 0) return;
-    const SeqRows sr = seq_rows(a.row_start, u.seq, a.n_rows);
+    const SeqRows sr = u.rows;
     const int n_used = sr.count * rep;
     // the longest first
-    const int first = kPromptRows * (int)(tiles_of(u.seq) - 1 - u.index), wave_first = first + 32 * wave;
+    const int first = kPromptRows * (int)(tiles_of(sr) - 1 - u.index), wave_first = first + 32 * wave;
     const int n_pos = min(first + kPromptRows - 1, n_used - 1) / rep + 1;               // positions that the workgroup's rows attend to
     const int wave_pos = wave_first < n_used ? min(wave_first + 31, n_used - 1) / rep + 1 : 0, wave_low = wave_first / rep;
     const uint16_t* kg = a.k + (size_t)sr.start * a.kv_stride + (size_t)grp * hd;

@@ -9,50 +9,65 @@
 namespace sd2 {
 
 struct SeqRows {
-    int start, count;
+    int start, count, pos0;  // first row, rows, position of the first row
 };
 
-__device__ __forceinline__ SeqRows seq_rows(const int32_t* __restrict__ row_start, int b, int n_rows) {
-    const int lo = min(max(row_start[b], 0), n_rows), hi = min(max(row_start[b + 1], lo), n_rows);
-    return {lo, hi - lo};
+// pos0 may be null: prompts
+__device__ __forceinline__ SeqRows seq_rows(const int32_t* __restrict__ row_start, const int32_t* __restrict__ pos0, int b, int n_rows) {
+    const int from = row_start[b], to = row_start[b + 1], first = pos0 ? pos0[b] : 0;
+    const int lo = min(max(from, 0), n_rows), hi = min(max(to, lo), n_rows);
+    return {lo, hi - lo, first};
 }
 
 struct SeqUnit {
     int seq;         // -1: past the last unit
     uint32_t index;  // unit inside the sequence
-    uint32_t before; // units of the sequences in front of it
+    SeqRows rows;
 };
 
-// The sequence that owns `unit`, where sequence b has count(b) units: 64 sequences a step, one in each lane.  All lanes of
-// the wavefront take part; the result is the same in all of them.
-template <typename F>
-__device__ __forceinline__ SeqUnit find_unit(uint32_t unit, int n_seq, F&& count) {
-    const int lane = threadIdx.x & 63;
-    uint32_t before = 0;
-    for (int base = 0; base < n_seq; base += 64) {
-        const int b = base + lane;
-        const uint32_t own = b < n_seq ? count(b) : 0u, incl = wave_incl_scan(own);
-        const uint64_t past = __ballot(before + incl > unit);
-        if (past) {
-            const int at = __builtin_ctzll(past);
-            const uint32_t first = before + (uint32_t)__builtin_amdgcn_readlane((int)(incl - own), at);
-            return {__builtin_amdgcn_readfirstlane(base + at), unit - first, first};
-        }
-        before += (uint32_t)__builtin_amdgcn_readlane((int)incl, 63);
-    }
-    return {-1, 0, before};
-}
+// The sequences as a wavefront goes through them, 64 a step, one in each lane; the first 64 are loaded once.  All lanes take part, and
+// what the functions return is the same in all of them.
+struct Sequences {
+    const int32_t *row_start, *pos0;
+    int n_seq, n_rows;
+    SeqRows first;
 
-// the sum of count(b) over all sequences
-template <typename F>
-__device__ __forceinline__ uint64_t total_units(int n_seq, F&& count) {
-    uint64_t sum = 0;
-    for (int base = 0; base < n_seq; base += 64) {
+    __device__ __forceinline__ Sequences(const int32_t* rs, const int32_t* p0, int n, int rows)
+        : row_start(rs), pos0(p0), n_seq(n), n_rows(rows), first(at(0)) {}
+
+    __device__ __forceinline__ SeqRows at(int base) const {
         const int b = base + (threadIdx.x & 63);
-        sum += (uint32_t)__builtin_amdgcn_readlane((int)wave_incl_scan(b < n_seq ? count(b) : 0u), 63);
+        return b < n_seq ? seq_rows(row_start, pos0, b, n_rows) : SeqRows{0, 0, 0};
     }
-    return sum;
-}
+
+    // the sum of count(sequence) over all sequences; count of no rows is zero
+    template <typename F>
+    __device__ __forceinline__ uint64_t total(F&& count) const {
+        uint64_t sum = 0;
+        for (int base = 0; base < n_seq; base += 64)
+            sum += (uint32_t)__builtin_amdgcn_readlane((int)wave_incl_scan(count(base ? at(base) : first)), 63);
+        return sum;
+    }
+
+    // the sequence that owns `unit`
+    template <typename F>
+    __device__ __forceinline__ SeqUnit find(uint32_t unit, F&& count) const {
+        uint32_t before = 0;
+        for (int base = 0; base < n_seq; base += 64) {
+            const SeqRows own = base ? at(base) : first;
+            const uint32_t n = count(own), incl = wave_incl_scan(n);
+            const uint64_t past = __ballot(before + incl > unit);
+            if (past) {
+                const int lane = __builtin_ctzll(past);
+                const SeqRows rows = {__builtin_amdgcn_readlane(own.start, lane), __builtin_amdgcn_readlane(own.count, lane),
+                                      __builtin_amdgcn_readlane(own.pos0, lane)};
+                return {__builtin_amdgcn_readfirstlane(base + lane), unit - before - (uint32_t)__builtin_amdgcn_readlane((int)(incl - n), lane), rows};
+            }
+            before += (uint32_t)__builtin_amdgcn_readlane((int)incl, 63);
+        }
+        return {-1, 0, {0, 0, 0}};
+    }
+};
 
 // the larger (the sum) of two lanes 32 apart, in both
 __device__ __forceinline__ float max_halves(float x) {

@@ -10,6 +10,8 @@
 // such that they follow one another -- and these are the second product's operand as they stand: weights never leave the registers.
 // Keys and values go from memory into LDS without passing through registers, a tile ahead; their 16-byte pieces are turned within a row
 // by the row's number, which spreads the reads over the banks.
+#include <type_traits>
+
 #include "sd2_internal.h"
 #include "sd2_rows.h"
 
@@ -40,6 +42,12 @@ __device__ __forceinline__ int val_place(int r, int c) {
     return 16 * (r * (D / 8) + (c ^ (D == 64 ? 4 * ((r >> 1) & 1) : 4 * (r & 3))));
 }
 
+// 16 bytes from base + offset of every lane to lds + 16 * lane.  As assembly, because the compiler waits for all such requests in front of
+// every transposing read of LDS: it cannot tell the buffers apart.  Nothing returns to registers; whoever reads the bytes waits first.
+__device__ __forceinline__ void load_to_lds(const void* base, uint32_t offset, uint32_t lds) {
+    asm volatile("s_mov_b32 m0, %2\n\ts_nop 0\n\tglobal_load_lds_dwordx4 %0, %1" ::"v"(offset), "s"(base), "s"(lds) : "memory");
+}
+
 template <int D>
 __global__ __launch_bounds__(64 * kPromptWaves, D == 256 ? 1 : 2) void prompt_attention_kernel(PromptArgs a) {
     constexpr int kTile = D == 256 ? 32 : 64, kRb = kTile / 32, kSteps = D / 16, kDb = D / 32, kBytes = kTile * D * 2;
@@ -48,12 +56,11 @@ __global__ __launch_bounds__(64 * kPromptWaves, D == 256 ? 1 : 2) void prompt_at
     const int tid = threadIdx.x, lane = tid & 63, wave = __builtin_amdgcn_readfirstlane(tid >> 6), n = lane & 31, h = lane >> 5;
     const int grp = blockIdx.x % a.n_kv, rep = a.rep, hd = a.head_dim;
     auto tiles_of = [&](const SeqRows& r) { return (uint32_t)(r.count * rep + kPromptRows - 1) / kPromptRows; };
-    const SeqUnit u = Sequences(a.row_start, nullptr, a.n_seq, a.n_rows).find(blockIdx.x / a.n_kv, tiles_of);
+    const SeqUnit u = Sequences(a.row_start, nullptr, a.n_seq, a.n_rows).find_largest_first(blockIdx.x / a.n_kv, tiles_of);
     if (u.seq < 0) return;
     const SeqRows sr = u.rows;
     const int n_used = sr.count * rep;
-    // the longest first
-    const int first = kPromptRows * (int)(tiles_of(sr) - 1 - u.index), wave_first = first + 32 * wave;
+    const int first = kPromptRows * (int)u.index, wave_first = first + 32 * wave;
     const int n_pos = min(first + kPromptRows - 1, n_used - 1) / rep + 1;               // positions that the workgroup's rows attend to
     const int wave_pos = wave_first < n_used ? min(wave_first + 31, n_used - 1) / rep + 1 : 0, wave_low = wave_first / rep;
     const uint16_t* kg = a.k + (size_t)sr.start * a.kv_stride + (size_t)grp * hd;
@@ -63,26 +70,26 @@ __global__ __launch_bounds__(64 * kPromptWaves, D == 256 ? 1 : 2) void prompt_at
         for (int i = tid; i < 2 * 2 * kBytes / 16; i += 64 * kPromptWaves) reinterpret_cast<u32x4*>(&smem[0][0][0])[i] = u32x4{0, 0, 0, 0};
         __syncthreads();
     }
-    // A tile's requests of this lane: rows r0, r0 + kStep, ..., the turned piece of each; no row past the sequence's last.
+    // A tile's requests of this lane: rows r0, r0 + kStep, ..., the turned piece of each, as byte offsets from the tile's first row.
     constexpr int kStep = 64 * kPromptWaves / (D / 8);
     const int r0 = (64 * wave + lane) / (D / 8), c0 = lane % (D / 8);
+    const uint32_t row_bytes = 2 * (uint32_t)a.kv_stride;
     auto request = [&](int base, int buf) __attribute__((always_inline)) {
         const uint16_t* kb = kg + (size_t)base * a.kv_stride;
         const uint16_t* vb = vg + (size_t)base * a.kv_stride;
-        const int last = sr.count - 1 - base;
+        const uint32_t to_lds = (uint32_t)(uintptr_t)(__attribute__((address_space(3))) uint8_t*)(&smem[buf][0][1024 * wave]);
+        auto pieces = [&](bool whole, bool all) __attribute__((always_inline)) {
 #pragma unroll
-        for (int i = 0; i < kCalls; ++i) {
-            const int r = r0 + kStep * i, slot = 1024 * (i * kPromptWaves + wave);
-            const uint32_t row = (uint32_t)min(r, last) * (uint32_t)a.kv_stride;
-            const uint32_t kc = (uint32_t)key_place<D>(r, c0) / 2 % D;
-            const uint32_t vc = (uint32_t)val_place<D>(r, c0) / 2 % D;
-            if (kc < (uint32_t)hd)
-                __builtin_amdgcn_global_load_lds((const __attribute__((address_space(1))) void*)(kb + (row + kc)),
-                                                 (__attribute__((address_space(3))) void*)(&smem[buf][0][slot]), 16, 0, 0);
-            if (vc < (uint32_t)hd)
-                __builtin_amdgcn_global_load_lds((const __attribute__((address_space(1))) void*)(vb + (row + vc)),
-                                                 (__attribute__((address_space(3))) void*)(&smem[buf][1][slot]), 16, 0, 0);
-        }
+            for (int i = 0; i < kCalls; ++i) {
+                const int r = r0 + kStep * i;
+                const uint32_t kc = (uint32_t)key_place<D>(r, c0) % (2 * D), vc = (uint32_t)val_place<D>(r, c0) % (2 * D);
+                const uint32_t at = (whole ? (uint32_t)r : (uint32_t)min(r, sr.count - 1 - base)) * row_bytes;  // no row past the sequence's last
+                if (all || kc < 2u * hd) load_to_lds(kb, at + kc, to_lds + 1024 * kPromptWaves * i);
+                if (all || vc < 2u * hd) load_to_lds(vb, at + vc, to_lds + kBytes + 1024 * kPromptWaves * i);
+            }
+        };
+        if (hd == D && base + kTile <= sr.count) pieces(true, true);
+        else pieces(false, false);
     };
     request(0, 0);
 
@@ -111,24 +118,28 @@ __global__ __launch_bounds__(64 * kPromptWaves, D == 256 ? 1 : 2) void prompt_at
     const int val_row = 8 * h + ((lane & 15) >> 2), val_piece = 2 * ((lane >> 4) & 1) + ((lane & 3) >> 1), val_byte = 8 * (lane & 1);
 
     int buf = 0, odd_from = 0x7fffffff;
-    for (int base = 0; base < n_pos; base += kTile, buf ^= 1) {
-        __syncthreads();  // the tile is there (the barrier waits for the wavefront's own requests), and nobody reads the other buffer
-        if (base + kTile < n_pos) request(base + kTile, buf ^ 1);
-        if (base >= wave_pos) continue;
+    auto tile = [&](int base, auto is_masked) __attribute__((always_inline)) {
+        constexpr bool masked = decltype(is_masked)::value;
         const uint8_t* kt = smem[buf][0];
         const uint8_t* vt = smem[buf][1];
         f32x16 s[kRb];
 #pragma unroll
-        for (int rb = 0; rb < kRb; ++rb) {
+        for (int rb = 0; rb < kRb; ++rb)
 #pragma unroll
             for (int i = 0; i < 16; ++i) s[rb][i] = 0.f;
 #pragma unroll
-            for (int i = 0; i < kSteps; ++i) {
+        for (int i = 0; i < kSteps; ++i)
+#pragma unroll
+            for (int rb = 0; rb < kRb; ++rb) {
                 const bf16x8 kf = *reinterpret_cast<const bf16x8*>(kt + key_place<D>(32 * rb + key_row, 2 * i + h));
                 s[rb] = __builtin_amdgcn_mfma_f32_32x32x16_bf16(kf, q[i], s[rb], 0, 0, 0);
             }
+        __builtin_amdgcn_sched_group_barrier(0x100, 6, 0);
+#pragma unroll
+        for (int i = 0; i < kSteps * kRb; ++i) {
+            __builtin_amdgcn_sched_group_barrier(0x008, 1, 0);
+            __builtin_amdgcn_sched_group_barrier(0x100, 1, 0);
         }
-        const bool masked = base + kTile - 1 > wave_low;
         if (masked) {
 #pragma unroll
             for (int rb = 0; rb < kRb; ++rb)
@@ -150,34 +161,6 @@ __global__ __launch_bounds__(64 * kPromptWaves, D == 256 ? 1 : 2) void prompt_at
 #pragma unroll
             for (int d = 0; d < kDb; ++d) o[d] *= f;
         }
-        bf16x8 p[kRb][2];  // positions 32 rb + 16 j + 8 h .. + 7
-#pragma unroll
-        for (int rb = 0; rb < kRb; ++rb)
-#pragma unroll
-            for (int j = 0; j < 2; ++j) {
-                float w[8];
-                Frag f;
-#pragma unroll
-                for (int e = 0; e < 8; ++e) {
-                    w[e] = __builtin_amdgcn_exp2f(__builtin_fmaf(s[rb][8 * j + e], a.scale, -m));
-                    l += w[e];
-                }
-#pragma unroll
-                for (int e = 0; e < 4; ++e) f.u[e] = pack_bf16(w[2 * e], w[2 * e + 1]);
-                p[rb][j] = f.v;
-            }
-        // operand of eight positions (32 rb + 16 j + 8 h ..) of dimension 32 db + n: two transposing reads of four rows
-        auto values = [&](int d, int rb, int j) __attribute__((always_inline)) {
-            Frag f;
-#pragma unroll
-            for (int e = 0; e < 2; ++e) {
-                const int r = 32 * rb + 16 * j + 4 * e + val_row;
-                const auto* src = (const __attribute__((address_space(3))) uint8_t*)vt + val_place<D>(r, 4 * d + val_piece) + val_byte;
-                const s16x4 x = __builtin_amdgcn_ds_read_tr16_b64_v4i16((__attribute__((address_space(3))) s16x4*)src);
-                reinterpret_cast<s16x4*>(&f)[e] = x;
-            }
-            return f;
-        };
         if (masked) {
             // A weight of zero times an infinity or NaN is NaN, also where the row does not attend to the position: from the first tile
             // on that holds such a value and is not attended to by all rows, values are added at the end, one position after the other.
@@ -190,14 +173,52 @@ __global__ __launch_bounds__(64 * kPromptWaves, D == 256 ? 1 : 2) void prompt_at
             }
             if (__any(largest >= 0xff000000u)) odd_from = min(odd_from, base);
         }
-        if (odd_from > base) {
+        // operand of eight positions (32 rb + 16 j + 8 h ..) of dimension 32 db + n: two transposing reads of four rows
+        auto values = [&](int d, int rb, int j) __attribute__((always_inline)) {
+            Frag f;
 #pragma unroll
-            for (int rb = 0; rb < kRb; ++rb)
+            for (int e = 0; e < 2; ++e) {
+                const int r = 32 * rb + 16 * j + 4 * e + val_row;
+                const auto* src = (const __attribute__((address_space(3))) uint8_t*)vt + val_place<D>(r, 4 * d + val_piece) + val_byte;
+                const s16x4 x = __builtin_amdgcn_ds_read_tr16_b64_v4i16((__attribute__((address_space(3))) s16x4*)src);
+                reinterpret_cast<s16x4*>(&f)[e] = x;
+            }
+            return f;
+        };
+        float sum[2] = {0.f, 0.f};
 #pragma unroll
-                for (int j = 0; j < 2; ++j)
+        for (int rb = 0; rb < kRb; ++rb)
 #pragma unroll
-                    for (int d = 0; d < kDb; ++d) o[d] = __builtin_amdgcn_mfma_f32_32x32x16_bf16(values(d, rb, j).v, p[rb][j], o[d], 0, 0, 0);
-        }
+            for (int j = 0; j < 2; ++j) {  // positions 32 rb + 16 j + 8 h .. + 7
+                float w[8];
+                Frag f;
+#pragma unroll
+                for (int e = 0; e < 8; ++e) {
+                    w[e] = __builtin_amdgcn_exp2f(__builtin_fmaf(s[rb][8 * j + e], a.scale, -m));
+                    sum[e & 1] += w[e];
+                }
+#pragma unroll
+                for (int e = 0; e < 4; ++e) f.u[e] = pack_bf16(w[2 * e], w[2 * e + 1]);
+                if (masked && odd_from <= base) continue;
+#pragma unroll
+                for (int d = 0; d < kDb; ++d) o[d] = __builtin_amdgcn_mfma_f32_32x32x16_bf16(values(d, rb, j).v, f.v, o[d], 0, 0, 0);
+            }
+        l += sum[0] + sum[1];
+    };
+    int base = 0;
+    auto next = [&]() __attribute__((always_inline)) {
+        __builtin_amdgcn_s_waitcnt(0x0F70);  // this wavefront's requests
+        asm volatile("" ::: "memory");
+        __syncthreads();  // everybody's: the tile is there, and nobody reads the other buffer
+        if (base + kTile < n_pos) request(base + kTile, buf ^ 1);
+    };
+    for (; base < n_pos && base + kTile - 1 <= wave_low; base += kTile, buf ^= 1) {  // all rows attend to all positions
+        next();
+        tile(base, std::false_type());
+    }
+    for (; base < n_pos; base += kTile, buf ^= 1) {
+        next();
+        if (base < wave_pos) tile(base, std::true_type());
     }
 #pragma unroll 1
     for (int pos = odd_from; pos <= token; ++pos) {

@@ -67,6 +67,34 @@ struct Sequences {
         }
         return {-1, 0, {0, 0, 0}};
     }
+
+    // The same units in another order: by their number inside their sequence, the largest first, so that what lasts longest starts first.
+    // (For up to 64 sequences; with more, sequence by sequence, as find has them, the largest first in each.)
+    template <typename F>
+    __device__ __forceinline__ SeqUnit find_largest_first(uint32_t unit, F&& count) const {
+        if (n_seq == 1 || n_seq > 64) {
+            SeqUnit u = find(unit, count);
+            u.index = count(u.rows) - 1 - u.index;
+            return u;
+        }
+        const uint32_t own = count(first);
+        // units whose number is at least `level`
+        auto from = [&](uint32_t level) { return (uint32_t)__builtin_amdgcn_readlane((int)wave_incl_scan(own > level ? own - level : 0u), 63); };
+        if (unit >= from(0)) return {-1, 0, {0, 0, 0}};
+        uint32_t level = 0, past = 1;
+        while (from(past) > unit) {
+            level = past;
+            past *= 2;
+        }
+        while (past - level > 1) {  // from(level) > unit >= from(past)
+            const uint32_t mid = (level + past) / 2;
+            if (from(mid) > unit) level = mid;
+            else past = mid;
+        }
+        const uint32_t incl = wave_incl_scan(own > level ? 1u : 0u);
+        const int lane = __builtin_ctzll(__ballot(incl > unit - from(past)));
+        return {lane, level, {__builtin_amdgcn_readlane(first.start, lane), __builtin_amdgcn_readlane(first.count, lane), 0}};
+    }
 };
 
 // the larger (the sum) of two lanes 32 apart, in both

@@ -10,6 +10,7 @@
 // such that they follow one another -- and these are the second product's operand as they stand: weights never leave the registers.
 // Keys and values go from memory into LDS without passing through registers, a tile ahead; their 16-byte pieces are turned within a row
 // by the row's number, which spreads the reads over the banks.
+#include <atomic>
 #include <type_traits>
 
 #include "sd2_internal.h"
@@ -17,8 +18,17 @@
 
 namespace sd2 {
 
-constexpr int kPromptWaves = 4;
-constexpr int kPromptRows = 32 * kPromptWaves;
+// A workgroup is G groups of 32 rows times T teams: a team is a wavefront for each group, and the teams take turns with the tiles of
+// positions.  T teams take a T-th of the steps one after the other, and their results meet in LDS.  Where rows alone do not fill the chip,
+// what counts is the chain of steps.
+constexpr int prompt_tile(int dim, int g) { return g == 1 || dim == 256 ? 32 : 64; }
+// Keys and values of each team's tile.  Teams of several wavefronts have two buffers, as all of them must be through with one before it can
+// be filled again; a wavefront alone asks for its next keys when the scores are there and for its next values when these have been read.
+constexpr int prompt_tiles(int dim, int g, int t) { return t * (g == 1 ? 1 : 2) * 2 * prompt_tile(dim, g) * dim * 2; }
+constexpr int prompt_meeting(int dim, int g, int t) { return t > 1 ? t * 32 * g * (dim + 4 + 2) * 4 : 0; }  // rows of dim + 4 sums, maxima and sums of weights
+constexpr int prompt_lds(int dim, int g, int t) {
+    return prompt_tiles(dim, g, t) > prompt_meeting(dim, g, t) ? prompt_tiles(dim, g, t) : prompt_meeting(dim, g, t);
+}
 
 typedef float f32x16 __attribute__((ext_vector_type(16)));
 typedef short s16x4 __attribute__((ext_vector_type(4)));
@@ -48,50 +58,69 @@ __device__ __forceinline__ void load_to_lds(const void* base, uint32_t offset, u
     asm volatile("s_mov_b32 m0, %2\n\ts_nop 0\n\tglobal_load_lds_dwordx4 %0, %1" ::"v"(offset), "s"(base), "s"(lds) : "memory");
 }
 
-template <int D>
-__global__ __launch_bounds__(64 * kPromptWaves, D == 256 ? 1 : 2) void prompt_attention_kernel(PromptArgs a) {
-    constexpr int kTile = D == 256 ? 32 : 64, kRb = kTile / 32, kSteps = D / 16, kDb = D / 32, kBytes = kTile * D * 2;
-    constexpr int kCalls = kBytes / (1024 * kPromptWaves);  // requests of a wavefront for a tile of keys (and of values)
-    __shared__ __attribute__((aligned(16))) uint8_t smem[2][2][kBytes];  // [buffer][keys, values]
+// the wait for all but the last n vector memory operations
+constexpr int wait_for(int n) { return 0x0F70 | (n & 15) | (n >> 4 << 14); }
+
+template <int D, int G, int T>
+__global__ __launch_bounds__(64 * G * T, G * T == 8 || D < 256 ? 2 : 1) void prompt_attention_kernel(PromptArgs a) {
+    constexpr int kTile = prompt_tile(D, G), kRb = kTile / 32, kSteps = D / 16, kDb = D / 32, kBytes = kTile * D * 2, kRows = 32 * G;
+    constexpr int kCalls = kBytes / (1024 * G);  // requests of a wavefront for a tile of keys (and of values)
+    constexpr int kAhead = kTile * T;            // positions from a team's tile to its next
+    extern __shared__ __attribute__((aligned(16))) uint8_t whole[];  // [team][kBuffers][keys, values][kBytes]
     const int tid = threadIdx.x, lane = tid & 63, wave = __builtin_amdgcn_readfirstlane(tid >> 6), n = lane & 31, h = lane >> 5;
     const int grp = blockIdx.x % a.n_kv, rep = a.rep, hd = a.head_dim;
-    auto tiles_of = [&](const SeqRows& r) { return (uint32_t)(r.count * rep + kPromptRows - 1) / kPromptRows; };
+    auto tiles_of = [&](const SeqRows& r) { return (uint32_t)(r.count * rep + kRows - 1) / kRows; };
     const SeqUnit u = Sequences(a.row_start, nullptr, a.n_seq, a.n_rows).find_largest_first(blockIdx.x / a.n_kv, tiles_of);
     if (u.seq < 0) return;
     const SeqRows sr = u.rows;
     const int n_used = sr.count * rep;
-    const int first = kPromptRows * (int)u.index, wave_first = first + 32 * wave;
-    const int n_pos = min(first + kPromptRows - 1, n_used - 1) / rep + 1;               // positions that the workgroup's rows attend to
+    const int team = wave / G, member = wave % G;
+    constexpr int kBuffers = G == 1 ? 1 : 2;
+    uint8_t* smem = whole + team * kBuffers * 2 * kBytes;
+    const int first = kRows * (int)u.index, wave_first = first + 32 * member;
+    const int n_pos = min(first + kRows - 1, n_used - 1) / rep + 1;               // positions that the workgroup's rows attend to
     const int wave_pos = wave_first < n_used ? min(wave_first + 31, n_used - 1) / rep + 1 : 0, wave_low = wave_first / rep;
     const uint16_t* kg = a.k + (size_t)sr.start * a.kv_stride + (size_t)grp * hd;
     const uint16_t* vg = a.v + (size_t)sr.start * a.kv_stride + (size_t)grp * hd;
 
     if (hd < D) {  // dimensions that the heads do not have: zero, and never written again
-        for (int i = tid; i < 2 * 2 * kBytes / 16; i += 64 * kPromptWaves) reinterpret_cast<u32x4*>(&smem[0][0][0])[i] = u32x4{0, 0, 0, 0};
+        for (int i = tid; i < prompt_tiles(D, G, T) / 16; i += 64 * G * T) reinterpret_cast<u32x4*>(whole)[i] = u32x4{0, 0, 0, 0};
         __syncthreads();
     }
     // A tile's requests of this lane: rows r0, r0 + kStep, ..., the turned piece of each, as byte offsets from the tile's first row.
-    constexpr int kStep = 64 * kPromptWaves / (D / 8);
-    const int r0 = (64 * wave + lane) / (D / 8), c0 = lane % (D / 8);
+    constexpr int kStep = 64 * G / (D / 8);
+    const int r0 = (64 * member + lane) / (D / 8), c0 = lane % (D / 8);
     const uint32_t row_bytes = 2 * (uint32_t)a.kv_stride;
-    auto request = [&](int base, int buf) __attribute__((always_inline)) {
+    auto request = [&](int base, int buf, auto which) __attribute__((always_inline)) {  // 1: keys, 2: values, 3: both
+        constexpr bool keys = decltype(which)::value & 1, values = decltype(which)::value & 2;
         const uint16_t* kb = kg + (size_t)base * a.kv_stride;
         const uint16_t* vb = vg + (size_t)base * a.kv_stride;
-        const uint32_t to_lds = (uint32_t)(uintptr_t)(__attribute__((address_space(3))) uint8_t*)(&smem[buf][0][1024 * wave]);
-        auto pieces = [&](bool whole, bool all) __attribute__((always_inline)) {
+        const uint32_t to_lds = (uint32_t)(uintptr_t)(__attribute__((address_space(3))) uint8_t*)(smem + 2 * buf * kBytes + 1024 * member);
+        auto pieces = [&](bool inside, bool all) __attribute__((always_inline)) {
 #pragma unroll
             for (int i = 0; i < kCalls; ++i) {
                 const int r = r0 + kStep * i;
                 const uint32_t kc = (uint32_t)key_place<D>(r, c0) % (2 * D), vc = (uint32_t)val_place<D>(r, c0) % (2 * D);
-                const uint32_t at = (whole ? (uint32_t)r : (uint32_t)min(r, sr.count - 1 - base)) * row_bytes;  // no row past the sequence's last
-                if (all || kc < 2u * hd) load_to_lds(kb, at + kc, to_lds + 1024 * kPromptWaves * i);
-                if (all || vc < 2u * hd) load_to_lds(vb, at + vc, to_lds + kBytes + 1024 * kPromptWaves * i);
+                const uint32_t at = (inside ? (uint32_t)r : (uint32_t)min(r, sr.count - 1 - base)) * row_bytes;  // no row past the sequence's last
+                if (keys && (all || kc < 2u * hd)) load_to_lds(kb, at + kc, to_lds + 1024 * G * i);
+                if (values && (all || vc < 2u * hd)) load_to_lds(vb, at + vc, to_lds + kBytes + 1024 * G * i);
             }
         };
         if (hd == D && base + kTile <= sr.count) pieces(true, true);
         else pieces(false, false);
     };
-    request(0, 0);
+    using Keys = std::integral_constant<int, 1>;
+    using Values = std::integral_constant<int, 2>;
+    using Both = std::integral_constant<int, 3>;
+    int base = kTile * team;
+    if (T == 1 || base < n_pos) {
+        if (G == 1) {
+            request(base, 0, Keys());
+            request(base, 0, Values());
+        } else {
+            request(base, 0, Both());
+        }
+    }
 
     // operand of the scores: row n, dimensions 16 step + 8 h .. + 7 (rows past the last repeat it; never written)
     const int row = min(wave_first + n, n_used - 1), token = row / rep, head = grp * rep + (row - token * rep);
@@ -120,8 +149,8 @@ __global__ __launch_bounds__(64 * kPromptWaves, D == 256 ? 1 : 2) void prompt_at
     int buf = 0, odd_from = 0x7fffffff;
     auto tile = [&](int base, auto is_masked) __attribute__((always_inline)) {
         constexpr bool masked = decltype(is_masked)::value;
-        const uint8_t* kt = smem[buf][0];
-        const uint8_t* vt = smem[buf][1];
+        const uint8_t* kt = smem + 2 * buf * kBytes;
+        const uint8_t* vt = kt + kBytes;
         f32x16 s[kRb];
 #pragma unroll
         for (int rb = 0; rb < kRb; ++rb)
@@ -139,6 +168,13 @@ __global__ __launch_bounds__(64 * kPromptWaves, D == 256 ? 1 : 2) void prompt_at
         for (int i = 0; i < kSteps * kRb; ++i) {
             __builtin_amdgcn_sched_group_barrier(0x008, 1, 0);
             __builtin_amdgcn_sched_group_barrier(0x100, 1, 0);
+        }
+        if constexpr (G == 1) {
+            if (base + kAhead < n_pos) {
+                __builtin_amdgcn_s_waitcnt(0xC07F);  // the keys have been read
+                asm volatile("" ::: "memory");
+                request(base + kAhead, 0, Keys());
+            }
         }
         if (masked) {
 #pragma unroll
@@ -160,6 +196,11 @@ __global__ __launch_bounds__(64 * kPromptWaves, D == 256 ? 1 : 2) void prompt_at
             l *= f;
 #pragma unroll
             for (int d = 0; d < kDb; ++d) o[d] *= f;
+        }
+        if constexpr (G == 1) {  // this tile's values: all but the keys just asked for
+            if (base + kAhead < n_pos) __builtin_amdgcn_s_waitcnt(wait_for(kCalls));
+            else __builtin_amdgcn_s_waitcnt(wait_for(0));
+            asm volatile("" ::: "memory");
         }
         if (masked) {
             // A weight of zero times an infinity or NaN is NaN, also where the row does not attend to the position: from the first tile
@@ -204,24 +245,39 @@ __global__ __launch_bounds__(64 * kPromptWaves, D == 256 ? 1 : 2) void prompt_at
                 for (int d = 0; d < kDb; ++d) o[d] = __builtin_amdgcn_mfma_f32_32x32x16_bf16(values(d, rb, j).v, f.v, o[d], 0, 0, 0);
             }
         l += sum[0] + sum[1];
+        if constexpr (G == 1) {
+            if (base + kAhead < n_pos) {
+                __builtin_amdgcn_s_waitcnt(0xC07F);  // the values have been read
+                asm volatile("" ::: "memory");
+                request(base + kAhead, 0, Values());
+            }
+        }
     };
-    int base = 0;
     auto next = [&]() __attribute__((always_inline)) {
-        __builtin_amdgcn_s_waitcnt(0x0F70);  // this wavefront's requests
-        asm volatile("" ::: "memory");
-        __syncthreads();  // everybody's: the tile is there, and nobody reads the other buffer
-        if (base + kTile < n_pos) request(base + kTile, buf ^ 1);
+        if constexpr (G == 1) {
+            __builtin_amdgcn_s_waitcnt(wait_for(kCalls));  // the keys: all but the values behind them
+            asm volatile("" ::: "memory");
+        } else {
+            __builtin_amdgcn_s_waitcnt(wait_for(0));  // this wavefront's requests
+            asm volatile("" ::: "memory");
+            __syncthreads();  // everybody's: the tile is there, and nobody reads the other buffer
+            if (base + kAhead < n_pos) request(base + kAhead, buf ^ 1, Both());
+        }
     };
-    for (; base < n_pos && base + kTile - 1 <= wave_low; base += kTile, buf ^= 1) {  // all rows attend to all positions
+    // the queries with the first tile: a wait of the compiler's for them would be one for what is asked for behind them as well
+    if (G == 1) __builtin_amdgcn_s_waitcnt(wait_for(0));
+    const int last = n_pos + kTile * team;           // as many steps for every team
+    for (; base < last && base + kTile - 1 <= wave_low; base += kAhead, buf ^= kBuffers - 1) {  // all rows attend to all positions
         next();
         tile(base, std::false_type());
     }
-    for (; base < n_pos; base += kTile, buf ^= 1) {
+    for (; base < last; base += kAhead, buf ^= kBuffers - 1) {
         next();
         if (base < wave_pos) tile(base, std::true_type());
     }
 #pragma unroll 1
     for (int pos = odd_from; pos <= token; ++pos) {
+        if (T > 1 && pos / kTile % T != team) continue;
         const uint16_t* key = kg + (size_t)pos * a.kv_stride;
         const uint16_t* query = a.q + (size_t)(sr.start + token) * a.q_stride + (size_t)head * hd;
         float dot = 0.f;
@@ -241,8 +297,47 @@ __global__ __launch_bounds__(64 * kPromptWaves, D == 256 ? 1 : 2) void prompt_at
                 o[d][4 * i + 3] += w * __uint_as_float(x.y & 0xffff0000u);
             }
     }
+    l = sum_halves(l);
+    if constexpr (T > 1) {  // the teams' results meet in LDS, 2 T threads a row
+        constexpr int kORow = D + 4;
+        float* sums = reinterpret_cast<float*>(whole);                        // [team][kRows][kORow]
+        float2* stats = reinterpret_cast<float2*>(sums + T * kRows * kORow);  // [team][kRows]
+        __syncthreads();
+        const int at = team * kRows + 32 * member + n;
+#pragma unroll
+        for (int d = 0; d < kDb; ++d)
+#pragma unroll
+            for (int i = 0; i < 4; ++i)
+                *reinterpret_cast<f32x4*>(sums + at * kORow + 32 * d + 8 * i + 4 * h) = f32x4{o[d][4 * i], o[d][4 * i + 1], o[d][4 * i + 2], o[d][4 * i + 3]};
+        if (h == 0) stats[at] = make_float2(m, l);
+        __syncthreads();
+        const int mine = tid / (2 * T), part = tid % (2 * T), row_of = first + mine;
+        if (row_of >= n_used) return;
+        float w[T], top = -3.0e38f, all = 0.f;
+#pragma unroll
+        for (int t = 0; t < T; ++t) top = fmaxf(top, stats[t * kRows + mine].x);
+#pragma unroll
+        for (int t = 0; t < T; ++t) {
+            const float2 st = stats[t * kRows + mine];
+            w[t] = __builtin_amdgcn_exp2f(st.x - top);
+            all += w[t] * st.y;
+        }
+        const float inv = 1.0f / all;
+        const int own = row_of / rep;
+        uint16_t* dst = a.out + ((size_t)(sr.start + own) * a.n_kv * rep + grp * rep + (row_of - own * rep)) * hd;
+#pragma unroll
+        for (int d = 4 * part; d < D; d += 8 * T) {
+            if (d >= hd) break;
+            f32x4 x = f32x4{0.f, 0.f, 0.f, 0.f};
+#pragma unroll
+            for (int t = 0; t < T; ++t) x += *reinterpret_cast<const f32x4*>(sums + (t * kRows + mine) * kORow + d) * w[t];
+            x *= inv;
+            *reinterpret_cast<uint2*>(dst + d) = make_uint2(pack_bf16(x[0], x[1]), pack_bf16(x[2], x[3]));
+        }
+        return;
+    }
     if (wave_first + n >= n_used) return;
-    const float inv = 1.0f / sum_halves(l);
+    const float inv = 1.0f / l;
     uint16_t* dst = a.out + ((size_t)(sr.start + token) * a.n_kv * rep + head) * hd + 4 * h;
 #pragma unroll
     for (int d = 0; d < kDb; ++d)
@@ -261,10 +356,34 @@ hipError_t launch_prompt_attention(const uint16_t* q, const uint16_t* k, const u
     const int rep = n_heads / n_kv;
     const PromptArgs a = {q, k, v, q_stride, kv_stride, row_start, n_seq, n_rows, n_kv, rep, head_dim,
                           (float)(1.4426950408889634 / sqrt((double)head_dim)), out};
-    const dim3 grid((unsigned)(((int64_t)n_rows * rep / kPromptRows + (n_seq < n_rows ? n_seq : n_rows)) * n_kv)), block(64 * kPromptWaves);
-    if (head_dim <= 64) hipLaunchKernelGGL(prompt_attention_kernel<64>, grid, block, 0, s, a);
-    else if (head_dim <= 128) hipLaunchKernelGGL(prompt_attention_kernel<128>, grid, block, 0, s, a);
-    else hipLaunchKernelGGL(prompt_attention_kernel<256>, grid, block, 0, s, a);
+    const int64_t seqs = n_seq < n_rows ? n_seq : n_rows, cus = device_cu_count();
+    auto units = [&](int g) { return ((int64_t)n_rows * rep / (32 * g) + seqs) * n_kv; };
+#define SD2_PROMPT(DIM, G, T)                                                                                                        \
+    do {                                                                                                                             \
+        static std::atomic<bool> raised{prompt_lds(DIM, G, T) <= 65536}; /* once (a warm-up call precedes any graph capture) */      \
+        if (!raised.load(std::memory_order_acquire)) {                                                                               \
+            const hipError_t e = hipFuncSetAttribute(reinterpret_cast<const void*>(&prompt_attention_kernel<DIM, G, T>),             \
+                                                     hipFuncAttributeMaxDynamicSharedMemorySize, prompt_lds(DIM, G, T));             \
+            if (e != hipSuccess) return e;                                                                                           \
+            raised.store(true, std::memory_order_release);                                                                           \
+        }                                                                                                                            \
+        hipLaunchKernelGGL((prompt_attention_kernel<DIM, G, T>), dim3((unsigned)units(G)), dim3(64 * G * T), prompt_lds(DIM, G, T), s, a); \
+    } while (0)
+    // Which kernel, by what the host knows (us, 24 query heads over 8 of 128 dimensions unless said otherwise; 32 rows a workgroup and four
+    // teams / 128 rows and two teams / 128 rows and one team):
+    //   300 tokens 8.1 / 10.9 / 11.5, 600 tokens 10.9 / 15.7 / 16.9, 2000 tokens with 12 heads over 2 28.3 / 33.4 / 39.0,
+    //   1024 tokens 21.6 / 21.6 / 23.9, 1500 tokens - / 29.0 / 34.1, eight prompts of 60 to 120 tokens 12.3 / 9.7 / 9.5: short prompts
+    //   have few steps to share, and more workgroups than run at once are not worth it there.
+    const bool few = units(1) <= 2 * cus || (units(1) <= 4 * cus && n_rows / seqs >= 256), some = units(4) <= 2 * cus;
+    if (head_dim <= 64 && few) SD2_PROMPT(64, 1, 4);
+    else if (head_dim <= 64 && some) SD2_PROMPT(64, 4, 2);
+    else if (head_dim <= 64) SD2_PROMPT(64, 4, 1);
+    else if (head_dim <= 128 && few) SD2_PROMPT(128, 1, 4);
+    else if (head_dim <= 128 && some) SD2_PROMPT(128, 4, 2);
+    else if (head_dim <= 128) SD2_PROMPT(128, 4, 1);
+    else if (few) SD2_PROMPT(256, 1, 4);
+    else SD2_PROMPT(256, 4, 1);
+#undef SD2_PROMPT
     return hipGetLastError();
 }
 

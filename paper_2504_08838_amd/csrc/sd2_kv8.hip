@@ -15,9 +15,9 @@ constexpr int kBlock = kKv8Block;
 // ------------------------------------------------------------------ rotary embedding, rounding, storing
 //
 // Workgroup (block of positions that a sequence's new rows touch, key/value head): the block's new keys and values and the
-// group's queries.  A thread owns four pairs of dimensions (i, i + D/2) of a row, so that a rotation needs nothing of another
-// lane; D/8 threads are a row, and rows that the workgroup has no use for take further heads.  The angle is position times
-// frequency in 64 bits, in revolutions: what is left after the whole ones are dropped has more bits than fp32 keeps.
+// group's queries.  A thread owns eight pairs of dimensions (i, i + D/2) of a row, so that a rotation needs nothing of another
+// lane; D/16 threads are a row, and threads that have no row of their own take further heads of the others'.  The angle is position
+// times frequency in 64 bits, in revolutions: what is left after the whole ones are dropped has more bits than fp32 keeps.
 
 // smallest e >= -100 with largest <= 448 * 2^e, as 2^e; largest: the magnitude bits of a finite bf16 value
 __device__ __forceinline__ float kv8_scale(uint32_t largest) {
@@ -37,25 +37,21 @@ __device__ __forceinline__ f32x4 unpack_e4m3(uint32_t c) {
     const f32x2 lo = __builtin_amdgcn_cvt_pk_f32_fp8((int)c, false), hi = __builtin_amdgcn_cvt_pk_f32_fp8((int)c, true);
     return f32x4{lo[0], lo[1], hi[0], hi[1]};
 }
-__device__ __forceinline__ f32x4 bf16x4_to_f32(uint2 p) {
-    return f32x4{__uint_as_float(p.x << 16), __uint_as_float(p.x & 0xffff0000u), __uint_as_float(p.y << 16), __uint_as_float(p.y & 0xffff0000u)};
+__device__ __forceinline__ f32x4 bf16x4_to_f32(uint32_t a, uint32_t b) {
+    return f32x4{__uint_as_float(a << 16), __uint_as_float(a & 0xffff0000u), __uint_as_float(b << 16), __uint_as_float(b & 0xffff0000u)};
 }
-// the largest magnitude among four bf16 values and `largest`, those that are not finite left out
-__device__ __forceinline__ uint32_t largest_finite(uint2 p, uint32_t largest) {
-    const uint32_t m[4] = {p.x & 0x7fffu, (p.x >> 16) & 0x7fffu, p.y & 0x7fffu, (p.y >> 16) & 0x7fffu};
-#pragma unroll
-    for (int i = 0; i < 4; ++i) largest = max(largest, m[i] < 0x7f80u ? m[i] : 0u);
-    return largest;
+// the largest magnitude among two bf16 values and `largest`, those that are not finite left out
+__device__ __forceinline__ uint32_t largest_finite(uint32_t pair, uint32_t largest) {
+    const uint32_t lo = pair & 0x7fffu, hi = (pair >> 16) & 0x7fffu;
+    return max(largest, max(lo < 0x7f80u ? lo : 0u, hi < 0x7f80u ? hi : 0u));
 }
 
 struct AppendArgs {
     Kv8Args c;
-    const float* qkv;
     const int32_t* row_start;
     const int32_t* pos0;
     int n_seq, n_rows, rep;
-    double log2_theta;
-    uint16_t* rows;
+    double log2_theta, step;  // step: ratio of the frequencies of neighbouring dimensions
 };
 
 // blocks that the rows of a sequence touch, positions first .. first + n - 1
@@ -65,11 +61,17 @@ __device__ __forceinline__ uint32_t touched_blocks(int64_t first, int n) {
 
 // P: passes of the workgroup over a full block's rows
 template <int P>
-__global__ __launch_bounds__(256) void kv8_append_kernel(AppendArgs a) {
+__global__ __launch_bounds__(256) void kv8_append_kernel(AppendArgs a, const float* __restrict__ qkv, uint16_t* __restrict__ out) {
     static_assert(kBlock == 32, "shifts by 5");
     __shared__ uint32_t largest[2];
     const int tid = threadIdx.x, grp = blockIdx.y, D = a.c.head_dim, half = D / 2;
-    const SeqUnit u = Sequences(a.row_start, a.pos0, a.n_seq, a.n_rows).find(blockIdx.x, [](const SeqRows& r) { return touched_blocks(r.pos0, r.count); });
+    const Sequences seqs(a.row_start, a.pos0, a.n_seq, a.n_rows);
+    const int lanes = D / 16, per_pass = 256 / lanes, sub = tid / lanes, j = tid - sub * lanes;  // threads of a row, rows of a pass
+    double freq[8];  // revolutions a position, while the lengths are on their way
+    freq[0] = exp2((double)(-16 * j) / D * a.log2_theta) * 0.15915494309189535;
+#pragma unroll
+    for (int i = 1; i < 8; ++i) freq[i] = freq[i - 1] * a.step;
+    const SeqUnit u = seqs.find(blockIdx.x, [](const SeqRows& r) { return touched_blocks(r.pos0, r.count); });
     if (u.seq < 0) return;
     const SeqRows sr = u.rows;
     const int64_t p0 = sr.pos0, block = (p0 >> 5) + u.index, lo_pos = block * kBlock;
@@ -85,70 +87,87 @@ __global__ __launch_bounds__(256) void kv8_append_kernel(AppendArgs a) {
         old_scale[0] = a.c.k_scale[at];
         old_scale[1] = a.c.v_scale[at];
     }
-    const int lanes = D / 8, per_pass = 256 / lanes;             // threads of a row, rows of a pass
     const int rows_at_once = min(n_here, per_pass), others = per_pass / rows_at_once;  // threads of a row for different heads
-    const int sub = tid / lanes, j = tid - sub * lanes, other = sub / rows_at_once, row_slot = sub - other * rows_at_once;
+    const int other = sub / rows_at_once, row_slot = sub - other * rows_at_once;
     const bool active = sub < per_pass && other < others;
+    const bool has_k = other == 0, has_v = other == (others > 1 ? 1 : 0);
     const int n_heads = a.c.n_kv * a.rep;
     const size_t width = (size_t)(n_heads + 2 * a.c.n_kv) * D;
-    const int k_col = (n_heads + grp) * D + 4 * j, v_col = k_col + a.c.n_kv * D;
-    double freq[4];  // revolutions a position
-#pragma unroll
-    for (int i = 0; i < 4; ++i) freq[i] = exp2(-2.0 * (4 * j + i) / D * a.log2_theta) * 0.15915494309189535;
+    const int k_col = (n_heads + grp) * D + 8 * j, v_col = k_col + a.c.n_kv * D, q_col = grp * a.rep * D + 8 * j;
     __syncthreads();
 
-    uint2 kept[2][P][2];  // the rounded keys and values of the thread's rows, low and high dimensions
+    u32x4 kept[2][P][2];  // the rounded keys and values of the thread's rows, low and high dimensions
     uint32_t most[2] = {0u, 0u};
 #pragma unroll
     for (int p = 0; p < P; ++p) {
         const int r = row_slot + p * rows_at_once;
-        kept[0][p][0] = kept[0][p][1] = kept[1][p][0] = kept[1][p][1] = make_uint2(0u, 0u);
-        if (!active || r >= n_here) continue;
-        f32x4 c, s;
 #pragma unroll
-        for (int i = 0; i < 4; ++i) {
+        for (int w = 0; w < 4; ++w) kept[w >> 1][p][w & 1] = u32x4{0, 0, 0, 0};
+        if (!active || r >= n_here) continue;
+        const float* src = qkv + (size_t)(row0 + r) * width;
+        uint16_t* dst = out + (size_t)(row0 + r) * width;
+        struct Pairs {
+            f32x4 x[2], y[2];
+        };
+        auto load = [&](int col) __attribute__((always_inline)) {
+            const f32x4 *lo = reinterpret_cast<const f32x4*>(src + col), *hi = reinterpret_cast<const f32x4*>(src + col + half);
+            return Pairs{{lo[0], lo[1]}, {hi[0], hi[1]}};
+        };
+        auto pack = [](const f32x4& u, const f32x4& v) __attribute__((always_inline)) {
+            return u32x4{pack_bf16(u[0], u[1]), pack_bf16(u[2], u[3]), pack_bf16(v[0], v[1]), pack_bf16(v[2], v[3])};
+        };
+        auto put = [&](int col, const u32x4& lo, const u32x4& hi) __attribute__((always_inline)) {
+            *reinterpret_cast<u32x4*>(dst + col) = lo;
+            *reinterpret_cast<u32x4*>(dst + col + half) = hi;
+        };
+        // the queries begin with the threads that have neither keys nor values; a head's rows are asked for a head ahead
+        int q = others > 2 ? (other + others - 2) % others : other;
+        Pairs kx, vx, qx;
+        if (has_k) kx = load(k_col);
+        if (has_v) vx = load(v_col);
+        if (q < a.rep) qx = load(q_col + q * D);
+        f32x4 c[2], s[2];
+#pragma unroll
+        for (int i = 0; i < 8; ++i) {
             const double turns = (double)(first + r) * freq[i];
             float sn, cs;
             sincospif((float)(2.0 * (turns - rint(turns))), &sn, &cs);
-            c[i] = cs;
-            s[i] = sn;
+            c[i >> 2][i & 3] = cs;
+            s[i >> 2][i & 3] = sn;
         }
-        const float* src = a.qkv + (size_t)(row0 + r) * width;
-        uint16_t* dst = a.rows + (size_t)(row0 + r) * width;
-        auto put = [&](int col, uint2 lo, uint2 hi) {
-            *reinterpret_cast<uint2*>(dst + col) = lo;
-            *reinterpret_cast<uint2*>(dst + col + half) = hi;
+        auto rotate = [&](const Pairs& v, u32x4& lo, u32x4& hi) __attribute__((always_inline)) {
+            lo = pack(v.x[0] * c[0] - v.y[0] * s[0], v.x[1] * c[1] - v.y[1] * s[1]);
+            hi = pack(v.y[0] * c[0] + v.x[0] * s[0], v.y[1] * c[1] + v.x[1] * s[1]);
         };
-        auto rotated = [&](int col, uint2& lo, uint2& hi) {
-            const f32x4 x = *reinterpret_cast<const f32x4*>(src + col), y = *reinterpret_cast<const f32x4*>(src + col + half);
-            const f32x4 l = x * c - y * s, h = y * c + x * s;
-            lo = make_uint2(pack_bf16(l[0], l[1]), pack_bf16(l[2], l[3]));
-            hi = make_uint2(pack_bf16(h[0], h[1]), pack_bf16(h[2], h[3]));
-        };
-        if (other == 0) {
-            rotated(k_col, kept[0][p][0], kept[0][p][1]);
+        if (has_k) {
+            rotate(kx, kept[0][p][0], kept[0][p][1]);
             put(k_col, kept[0][p][0], kept[0][p][1]);
-            most[0] = largest_finite(kept[0][p][1], largest_finite(kept[0][p][0], most[0]));
         }
-        if (other == (others > 1 ? 1 : 0)) {
-            const f32x4 x = *reinterpret_cast<const f32x4*>(src + v_col), y = *reinterpret_cast<const f32x4*>(src + v_col + half);
-            kept[1][p][0] = make_uint2(pack_bf16(x[0], x[1]), pack_bf16(x[2], x[3]));
-            kept[1][p][1] = make_uint2(pack_bf16(y[0], y[1]), pack_bf16(y[2], y[3]));
+        if (has_v) {
+            kept[1][p][0] = pack(vx.x[0], vx.x[1]);
+            kept[1][p][1] = pack(vx.y[0], vx.y[1]);
             put(v_col, kept[1][p][0], kept[1][p][1]);
-            most[1] = largest_finite(kept[1][p][1], largest_finite(kept[1][p][0], most[1]));
         }
-        // the queries begin with the threads that have neither keys nor values
-        for (int q = others > 2 ? (other + others - 2) % others : other; q < a.rep; q += others) {
-            const int col = (grp * a.rep + q) * D + 4 * j;
-            uint2 lo, hi;
-            rotated(col, lo, hi);
+#pragma unroll
+        for (int w = 0; w < 4; ++w)
+#pragma unroll
+            for (int e = 0; e < 4; ++e) most[w >> 1] = largest_finite(kept[w >> 1][p][w & 1][e], most[w >> 1]);
+        while (q < a.rep) {
+            const int col = q_col + q * D;
+            const Pairs now = qx;
+            q += others;
+            if (q < a.rep) qx = load(q_col + q * D);
+            u32x4 lo, hi;
+            rotate(now, lo, hi);
             put(col, lo, hi);
         }
     }
     if (!stored) return;
 #pragma unroll
-    for (int w = 0; w < 2; ++w)
-        if (most[w]) atomicMax(&largest[w], most[w]);
+    for (int w = 0; w < 2; ++w) {
+        const uint32_t all = wave_max(most[w]);
+        if ((tid & 63) == 0) atomicMax(&largest[w], all);
+    }
     __syncthreads();
 #pragma unroll
     for (int w = 0; w < 2; ++w) {
@@ -160,14 +179,17 @@ __global__ __launch_bounds__(256) void kv8_append_kernel(AppendArgs a) {
             for (int i = tid; i < n_old * D / 4; i += 256) word[i] = pack_e4m3(unpack_e4m3(word[i]) * ratio);
         }
         if (tid == 0) (w ? a.c.v_scale : a.c.k_scale)[at] = scale;
-        if (!active || other != (w && others > 1 ? 1 : 0)) continue;
+        if (!active || !(w ? has_v : has_k)) continue;
 #pragma unroll
         for (int p = 0; p < P; ++p) {
             const int r = row_slot + p * rows_at_once;
             if (r >= n_here) continue;
-            uint8_t* dst = codes + (size_t)((int)(first - lo_pos) + r) * D + 4 * j;
-            *reinterpret_cast<uint32_t*>(dst) = pack_e4m3(bf16x4_to_f32(kept[w][p][0]) * inv);
-            *reinterpret_cast<uint32_t*>(dst + half) = pack_e4m3(bf16x4_to_f32(kept[w][p][1]) * inv);
+            uint8_t* dst = codes + (size_t)((int)(first - lo_pos) + r) * D + 8 * j;
+#pragma unroll
+            for (int e = 0; e < 2; ++e) {
+                const u32x4 x = kept[w][p][e];
+                *reinterpret_cast<uint2*>(dst + e * half) = make_uint2(pack_e4m3(bf16x4_to_f32(x[0], x[1]) * inv), pack_e4m3(bf16x4_to_f32(x[2], x[3]) * inv));
+            }
         }
     }
 }
@@ -176,13 +198,11 @@ hipError_t launch_kv8_append(const Kv8Args& c, const float* qkv, int n_heads, co
                              int n_rows, double theta, uint16_t* rows, hipStream_t s) {
     if (c.head_dim < 16 || c.head_dim > 256 || c.head_dim % 16) return hipErrorInvalidValue;
     if (n_rows == 0 || n_seq == 0) return hipSuccess;
-    const AppendArgs a = {c, qkv, row_start, pos0, n_seq, n_rows, n_heads / c.n_kv, log2(theta), rows};
+    const AppendArgs a = {c, row_start, pos0, n_seq, n_rows, n_heads / c.n_kv, log2(theta), exp2(-2.0 / c.head_dim * log2(theta))};
     // n rows touch at most (n + 62) / 32 blocks
     const dim3 grid((unsigned)(n_rows / kBlock + 2 * (n_seq < n_rows ? n_seq : n_rows)), (unsigned)c.n_kv);
-    const int per_pass = 256 / (c.head_dim / 8);
-    if (per_pass >= 32) hipLaunchKernelGGL(kv8_append_kernel<1>, grid, dim3(256), 0, s, a);
-    else if (per_pass >= 16) hipLaunchKernelGGL(kv8_append_kernel<2>, grid, dim3(256), 0, s, a);
-    else hipLaunchKernelGGL(kv8_append_kernel<4>, grid, dim3(256), 0, s, a);
+    if (c.head_dim <= 128) hipLaunchKernelGGL(kv8_append_kernel<1>, grid, dim3(256), 0, s, a, qkv, rows);
+    else hipLaunchKernelGGL(kv8_append_kernel<2>, grid, dim3(256), 0, s, a, qkv, rows);
     return hipGetLastError();
 }
 

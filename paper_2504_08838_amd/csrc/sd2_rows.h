@@ -116,4 +116,18 @@ __device__ __forceinline__ float sum_quarters(float x) {
     return __uint_as_float(r[0]) + __uint_as_float(r[1]);
 }
 
+// the largest over all lanes, in all of them
+__device__ __forceinline__ uint32_t wave_max(uint32_t x) {
+#define SD2_ROW_MAX(ctrl) x = max(x, (uint32_t)__builtin_amdgcn_update_dpp(0, (int)x, ctrl, 0xf, 0xf, true))
+    SD2_ROW_MAX(0x121);  // row_ror:1
+    SD2_ROW_MAX(0x122);  // row_ror:2
+    SD2_ROW_MAX(0x124);  // row_ror:4
+    SD2_ROW_MAX(0x128);  // row_ror:8
+#undef SD2_ROW_MAX
+    const auto r16 = __builtin_amdgcn_permlane16_swap(x, x, false, false);
+    x = max(r16[0], r16[1]);
+    const auto r32 = __builtin_amdgcn_permlane32_swap(x, x, false, false);
+    return max(r32[0], r32[1]);
+}
+
 }  // namespace sd2

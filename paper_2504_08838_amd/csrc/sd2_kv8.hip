@@ -3,8 +3,6 @@
 // A block of 32 positions of one head shares a scale, a power of two: a product with it is exact in fp32, bf16 and the matrix
 // instructions, so quantising rounds once, a block that is still open is brought to a larger scale by its exponents alone, and
 // attention applies scales where they cost nothing (keys: to the score; values: in the conversion to bf16).
-#include <atomic>
-
 #include "sd2_internal.h"
 #include "sd2_rows.h"
 
@@ -710,15 +708,6 @@ hipError_t launch_kv8_attention(const Kv8Args& c, const uint16_t* q, int64_t q_s
                     (float)(1.4426950408889634 / sqrt((double)c.head_dim)), out, static_cast<float*>(ws),
                     reinterpret_cast<float2*>(static_cast<uint8_t*>(ws) + p.stat_off),
                     reinterpret_cast<uint2*>(static_cast<uint8_t*>(ws) + p.join_off)};
-    if (kv8_lds(p.dim) > 65536) {
-        static std::atomic<bool> raised{false};  // once, at the first call (a warm-up call precedes any graph capture)
-        if (!raised.load(std::memory_order_acquire)) {
-            const hipError_t e = hipFuncSetAttribute(reinterpret_cast<const void*>(&kv8_attention_kernel<256, 1>),
-                                                     hipFuncAttributeMaxDynamicSharedMemorySize, kv8_lds(256));
-            if (e != hipSuccess) return e;
-            raised.store(true, std::memory_order_release);
-        }
-    }
     // row tiles that these rows can have
     const uint64_t tiles = (uint64_t)n_rows * rep / (16 * p.nr) + (uint64_t)(n_seq < n_rows ? n_seq : n_rows);
     const uint64_t most = (uint64_t)n_seq * p.tiles;
@@ -729,6 +718,9 @@ hipError_t launch_kv8_attention(const Kv8Args& c, const uint16_t* q, int64_t q_s
     const dim3 join((unsigned)(wide ? pairs : (pairs + 3) / 4));
 #define SD2_KV8(DIM, R)                                                                                                   \
     if (p.dim == DIM && p.nr == R) {                                                                                      \
+        static std::atomic<uint64_t> done{0};                                                                             \
+        const hipError_t e = allow_lds(reinterpret_cast<const void*>(&kv8_attention_kernel<DIM, R>), kv8_lds(DIM), done); \
+        if (e != hipSuccess) return e;                                                                                    \
         hipLaunchKernelGGL((kv8_attention_kernel<DIM, R>), grid, dim3(64 * kAttWaves), kv8_lds(DIM), s, a);               \
         if (c.max_pos > kAttSpan && wide) hipLaunchKernelGGL((kv8_combine_kernel<DIM, R, 4>), join, dim3(256), 0, s, a);  \
         if (c.max_pos > kAttSpan && !wide) hipLaunchKernelGGL((kv8_combine_kernel<DIM, R, 1>), join, dim3(256), 0, s, a); \

@@ -10,7 +10,6 @@
 // such that they follow one another -- and these are the second product's operand as they stand: weights never leave the registers.
 // Keys and values go from memory into LDS without passing through registers, a tile ahead; their 16-byte pieces are turned within a row
 // by the row's number, which spreads the reads over the banks.
-#include <atomic>
 #include <type_traits>
 
 #include "sd2_internal.h"
@@ -360,13 +359,9 @@ hipError_t launch_prompt_attention(const uint16_t* q, const uint16_t* k, const u
     auto units = [&](int g) { return ((int64_t)n_rows * rep / (32 * g) + seqs) * n_kv; };
 #define SD2_PROMPT(DIM, G, T)                                                                                                        \
     do {                                                                                                                             \
-        static std::atomic<bool> raised{prompt_lds(DIM, G, T) <= 65536}; /* once (a warm-up call precedes any graph capture) */      \
-        if (!raised.load(std::memory_order_acquire)) {                                                                               \
-            const hipError_t e = hipFuncSetAttribute(reinterpret_cast<const void*>(&prompt_attention_kernel<DIM, G, T>),             \
-                                                     hipFuncAttributeMaxDynamicSharedMemorySize, prompt_lds(DIM, G, T));             \
-            if (e != hipSuccess) return e;                                                                                           \
-            raised.store(true, std::memory_order_release);                                                                           \
-        }                                                                                                                            \
+        static std::atomic<uint64_t> done{0};                                                                                        \
+        const hipError_t e = allow_lds(reinterpret_cast<const void*>(&prompt_attention_kernel<DIM, G, T>), prompt_lds(DIM, G, T), done); \
+        if (e != hipSuccess) return e;                                                                                               \
         hipLaunchKernelGGL((prompt_attention_kernel<DIM, G, T>), dim3((unsigned)units(G)), dim3(64 * G * T), prompt_lds(DIM, G, T), s, a); \
     } while (0)
     // Which kernel, by what the host knows (us, 24 query heads over 8 of 128 dimensions unless said otherwise; 32 rows a workgroup and four

@@ -4,9 +4,24 @@
 // finds its own work by a prefix sum over the sequences.  Offsets are clamped to the rows that the call has, and whatever
 // they hold, no kernel reads or writes outside its buffers.
 #pragma once
+#include <atomic>
+
 #include "sd2_device.h"
 
 namespace sd2 {
+
+// Lets a kernel have more than 64 KiB of LDS.  `done`: the devices (bit by number) that have been told so for this kernel.
+inline hipError_t allow_lds(const void* kernel, int bytes, std::atomic<uint64_t>& done) {
+    if (bytes <= 65536) return hipSuccess;
+    int device = 0;
+    hipError_t e = hipGetDevice(&device);
+    if (e != hipSuccess) return e;
+    const uint64_t bit = (uint64_t)1 << (device & 63);
+    if (done.load(std::memory_order_acquire) & bit) return hipSuccess;
+    e = hipFuncSetAttribute(kernel, hipFuncAttributeMaxDynamicSharedMemorySize, bytes);
+    if (e == hipSuccess) done.fetch_or(bit, std::memory_order_release);
+    return e;
+}
 
 struct SeqRows {
     int start, count, pos0;  // first row, rows, position of the first row

@@ -381,20 +381,21 @@ KV8_BLOCK = 32  # positions that share a scale
 def kv8_cache_init(k_ptr, v_ptr, k_scale_ptr, v_scale_ptr, n_slots, n_kv, max_pos, head_dim):
     """Device pointers of the codes (uint8 [n_slots][n_kv][max_pos][head_dim]) and scales (fp32 [n_slots][n_kv][max_pos / 32])."""
     c = Kv8Cache()
-    _check(lib().sd2_kv8_cache_init(C.byref(c), C.c_void_p(k_ptr), C.c_void_p(v_ptr), C.c_void_p(k_scale_ptr), C.c_void_p(v_scale_ptr),
+    _check(lib().sd2_kv8_cache_init(C.byref(c), k_ptr, v_ptr, k_scale_ptr, v_scale_ptr,
                                     n_slots, n_kv, max_pos, head_dim), "sd2_kv8_cache_init")
     return c
 
 
+# The pointers of these calls go to ctypes as they are: the declared argument types convert them, and a call takes a microsecond less.
 def kv8_append(cache, qkv_ptr, n_heads, row_start_ptr, pos0_ptr, n_seq, n_rows, rope_theta, rows_bf16_ptr, stream=0):
-    _check(lib().sd2_kv8_append(C.byref(cache), C.c_void_p(qkv_ptr), n_heads, C.c_void_p(row_start_ptr), C.c_void_p(pos0_ptr), n_seq, n_rows,
-                                float(rope_theta), C.c_void_p(rows_bf16_ptr), C.c_void_p(stream)), "sd2_kv8_append")
+    _check(lib().sd2_kv8_append(C.byref(cache), qkv_ptr, n_heads, row_start_ptr, pos0_ptr, n_seq, n_rows,
+                                float(rope_theta), rows_bf16_ptr, stream), "sd2_kv8_append")
 
 
 def prompt_attention(q_ptr, k_ptr, v_ptr, q_stride, kv_stride, row_start_ptr, n_seq, n_rows, n_heads, n_kv, head_dim, out_ptr, stream=0):
     """Strides in values; out: bf16 [n_rows][n_heads * head_dim]."""
-    _check(lib().sd2_prompt_attention(C.c_void_p(q_ptr), C.c_void_p(k_ptr), C.c_void_p(v_ptr), q_stride, kv_stride, C.c_void_p(row_start_ptr),
-                                      n_seq, n_rows, n_heads, n_kv, head_dim, C.c_void_p(out_ptr), C.c_void_p(stream)),
+    _check(lib().sd2_prompt_attention(q_ptr, k_ptr, v_ptr, q_stride, kv_stride, row_start_ptr,
+                                      n_seq, n_rows, n_heads, n_kv, head_dim, out_ptr, stream),
            "sd2_prompt_attention")
 
 
@@ -405,8 +406,8 @@ def kv8_attention_workspace_size(cache, n_heads, n_seq, max_new):
 
 
 def kv8_attention(cache, q_ptr, q_stride, n_heads, row_start_ptr, pos0_ptr, n_seq, n_rows, max_new, out_ptr, ws_ptr, ws_bytes, stream=0):
-    _check(lib().sd2_kv8_attention(C.byref(cache), C.c_void_p(q_ptr), q_stride, n_heads, C.c_void_p(row_start_ptr), C.c_void_p(pos0_ptr), n_seq,
-                                   n_rows, max_new, C.c_void_p(out_ptr), C.c_void_p(ws_ptr), ws_bytes, C.c_void_p(stream)),
+    _check(lib().sd2_kv8_attention(C.byref(cache), q_ptr, q_stride, n_heads, row_start_ptr, pos0_ptr, n_seq,
+                                   n_rows, max_new, out_ptr, ws_ptr, ws_bytes, stream),
            "sd2_kv8_attention")
 
 

@@ -216,6 +216,8 @@ hipError_t launch_kv8_append(const Kv8Args& c, const float* qkv, int n_heads, co
 constexpr int kAttWaves = 4;
 constexpr int kAttSpan = 32 * kAttWaves;  // positions of the workgroup's tiles side by side
 
+constexpr uint32_t kRest = 0x80000000u;
+
 struct Kv8AttArgs {
     Kv8Args c;
     const uint16_t* q;
@@ -229,7 +231,7 @@ struct Kv8AttArgs {
     uint16_t* out;
     float* part;   // [units][key/value heads][16 NR][D]
     float2* stat;  // [units][key/value heads][16 NR]: running maximum (of scores times log2 e) and sum
-    uint2* join;   // [sequences][max_new][query heads]: the row's first unit, and its number of stretches
+    uint4* join;   // [sequences][max_new][query heads]: first unit of a row, its whole stretches (kRest: and a shorter one), the unit of that
 };
 
 // How a sequence is cut: row tiles and stretches of positions.  The stretch is the same for all sequences, so that workgroups are
@@ -249,12 +251,13 @@ __device__ __forceinline__ SeqCut seq_cut(const Kv8AttArgs& a, const SeqRows& r)
 }
 
 // Spans of a stretch, the same for all sequences.  With few row tiles: as few spans as let all stretches run side by side (64 rows against
-// 500 to 4000 positions, four sequences: 24 us with 512 stretches for 512 places, 26 with 448, 32 with 320 and with 832).  With more, twice
-// as many stretches as places: sequences differ in length, and short stretches fill the gaps (59 sequences of 14 to 16000 positions: 114 us
-// with a stretch a place, 104 with two, 106 with four).  A sequence of more than 128 spans is not cut into single ones, as what they
-// leave has to be joined (30000 positions: 17.6 us cut into single spans, 14.8 into pairs).
+// 500 to 4000 positions, four sequences: 24 us with 512 stretches for 512 places, 26 with 448, 32 with 320 and with 832).  With many, twice
+// as many stretches as places, whole ones first and what is left of each sequence behind them: sequences differ in length, and the short
+// ones fill the gaps (59 sequences of 14 to 16000 positions: 101 us; 114 with a stretch a place, 103 with three; 103 with two in the
+// sequences' order).  A sequence of more than 128 spans is not cut into single ones, as what they leave has to be joined (30000
+// positions: 17.6 us cut into single spans, 14.8 into pairs).
 template <int ROWS>
-__device__ __forceinline__ uint32_t stretch_of(const Kv8AttArgs& a, const Sequences& seqs) {
+__device__ __forceinline__ uint32_t stretch_of(const Kv8AttArgs& a, const Sequences& seqs, bool& many) {
     const uint64_t all = seqs.total([&](const SeqRows& r) {
         const SeqCut s = seq_cut<ROWS>(a, r);
         return s.tiles * s.spans;
@@ -262,7 +265,8 @@ __device__ __forceinline__ uint32_t stretch_of(const Kv8AttArgs& a, const Sequen
     const uint32_t tiles = (uint32_t)seqs.total([&](const SeqRows& r) { return seq_cut<ROWS>(a, r).tiles; });
     const uint32_t places = (uint32_t)a.places;
     auto share = [&](uint32_t n) { return (uint32_t)((all + n - 1) / n); };
-    if (2 * tiles > places) return max(share(2 * places), 1u);
+    many = 2 * tiles > places;
+    if (many) return max(share(2 * places), 1u);
     uint32_t stretch = max(share(places), all > 128 * (uint64_t)tiles ? 2u : 1u);
     const uint32_t enough = share(places - tiles);  // a sequence's last stretch may be short: no more than one for each row tile
     while (stretch < enough && seqs.total([&](const SeqRows& r) {
@@ -328,16 +332,23 @@ __global__ __launch_bounds__(64 * kAttWaves, kv8_waves(D, NR)) void kv8_attentio
     const int grp = blockIdx.x % a.c.n_kv;
     const uint32_t unit = blockIdx.x / a.c.n_kv;
     const Sequences seqs(a.row_start, a.pos0, a.n_seq, a.n_rows);
-    const uint32_t stretch = stretch_of<kRows>(a, seqs);
-    const SeqUnit u = seqs.find(unit, [&](const SeqRows& r) {
+    bool many;
+    const uint32_t stretch = stretch_of<kRows>(a, seqs, many);
+    // with many, whole stretches first, then what is left of each sequence
+    auto whole = [&](const SeqRows& r) {
         const SeqCut s = seq_cut<kRows>(a, r);
-        return s.tiles * ((s.spans + stretch - 1) / stretch);
+        return s.tiles * ((many ? s.spans : s.spans + stretch - 1) / stretch);
+    };
+    const uint32_t n_whole = many ? (uint32_t)seqs.total(whole) : ~0u;
+    const SeqUnit u = unit < n_whole ? seqs.find(unit, whole) : seqs.find(unit - n_whole, [&](const SeqRows& r) {
+        const SeqCut s = seq_cut<kRows>(a, r);
+        return s.spans % stretch ? s.tiles : 0u;
     });
     if (u.seq < 0) return;
     const SeqCut sc = seq_cut<kRows>(a, u.rows);
     const int64_t pos0 = u.rows.pos0;
-    const uint32_t cuts = (sc.spans + stretch - 1) / stretch;
-    const int tile = (int)(u.index / cuts), cut = (int)(u.index % cuts);
+    const uint32_t cuts = (sc.spans + stretch - 1) / stretch, cuts_whole = many ? sc.spans / stretch : cuts;
+    const int tile = (int)(unit < n_whole ? u.index / cuts_whole : u.index), cut = (int)(unit < n_whole ? u.index % cuts_whole : cuts_whole);
     const int D_used = a.c.head_dim, rep = a.rep, n_used = sc.count * rep;  // rows of the sequence
     const int first = kRows * tile;
     // positions of this workgroup, up to the last that its last row attends to
@@ -573,7 +584,9 @@ __global__ __launch_bounds__(64 * kAttWaves, kv8_waves(D, NR)) void kv8_attentio
             const size_t slot = ((size_t)unit * a.c.n_kv + grp) * kRows + 16 * t + r16;
             if ((tid & 15) == 0) {
                 if (cuts > 1) a.stat[slot] = make_float2(top, all);
-                if (cut == 0) a.join[((size_t)u.seq * a.max_new + token) * (a.c.n_kv * rep) + grp * rep + (row - token * rep)] = make_uint2(unit, cuts);
+                uint4* join = a.join + ((size_t)u.seq * a.max_new + token) * (a.c.n_kv * rep) + grp * rep + (row - token * rep);
+                if (cut == 0) *reinterpret_cast<uint2*>(join) = make_uint2(unit, cuts_whole | (cuts > cuts_whole ? kRest : 0u));
+                if (unit >= n_whole) join->z = unit;
             }
 #pragma unroll
             for (int d = 4 * (tid & 15); d < D; d += 64) {
@@ -603,14 +616,16 @@ __global__ __launch_bounds__(256) void kv8_combine_kernel(Kv8AttArgs a) {
     const uint32_t item = blockIdx.x * (4 / W) + (W > 1 ? 0u : (uint32_t)__builtin_amdgcn_readfirstlane((int)threadIdx.x >> 6));
     const uint32_t h = item % (uint32_t)n_heads, row = item / (uint32_t)n_heads;  // row: sequence times max_new + token
     if (row >= (uint32_t)a.n_seq * (uint32_t)a.max_new) return;
-    const uint2 join = a.join[(size_t)row * n_heads + h];
+    const uint4 join = a.join[(size_t)row * n_heads + h];
     const int seq = (int)(row / (uint32_t)a.max_new), token = (int)(row % (uint32_t)a.max_new);
     const SeqRows sr = seq_rows(a.row_start, a.pos0, seq, a.n_rows);
     if (token >= sr.count) return;  // nobody wrote the entry
-    const uint32_t cuts = (uint32_t)__builtin_amdgcn_readfirstlane((int)join.y), unit0 = (uint32_t)__builtin_amdgcn_readfirstlane((int)join.x);
-    if (cuts <= 1 || unit0 >= a.bound || cuts > a.bound - unit0) return;
+    const uint32_t unit0 = (uint32_t)__builtin_amdgcn_readfirstlane((int)join.x), wholes = (uint32_t)__builtin_amdgcn_readfirstlane((int)(join.y & ~kRest));
+    const uint32_t has_rest = (uint32_t)__builtin_amdgcn_readfirstlane((int)(join.y >> 31)), rest = (uint32_t)__builtin_amdgcn_readfirstlane((int)join.z);
+    const uint32_t cuts = wholes + has_rest;
+    if (cuts <= 1 || unit0 >= a.bound || wholes > a.bound - unit0 || (has_rest && rest >= a.bound)) return;
     const int grp = (int)h / a.rep, local = (token * a.rep + ((int)h - grp * a.rep)) % kRows;
-    const size_t slot0 = ((size_t)unit0 * a.c.n_kv + grp) * kRows + local, step = (size_t)a.c.n_kv * kRows;
+    auto slot_of = [&](uint32_t i) { return ((size_t)(i < wholes ? unit0 + i : rest) * a.c.n_kv + grp) * kRows + local; };
     const int side = tid / kLanes, d = 4 * (tid % kLanes);
     const bool used = d < a.c.head_dim;
     float top = -3.0e38f, all = 0.f;
@@ -626,8 +641,8 @@ __global__ __launch_bounds__(256) void kv8_combine_kernel(Kv8AttArgs a) {
             st[e] = make_float2(-3.0e38f, 0.f);
             v[e] = f32x4{0.f, 0.f, 0.f, 0.f};
             if (at < cuts) {
-                st[e] = a.stat[slot0 + at * step];
-                if (used) v[e] = *reinterpret_cast<const f32x4*>(a.part + (slot0 + at * step) * D + d);
+                st[e] = a.stat[slot_of(at)];
+                if (used) v[e] = *reinterpret_cast<const f32x4*>(a.part + slot_of(at) * D + d);
             }
         }
 #pragma unroll
@@ -693,8 +708,8 @@ Kv8Plan kv8_plan(int n_heads, int n_kv, int head_dim, int n_seq, int max_new) {
     p.bound = 2 * (uint32_t)p.places + (uint32_t)n_seq * (uint32_t)p.tiles;
     const size_t slots = (size_t)p.bound * kv * 16 * p.nr;
     p.stat_off = slots * p.dim * sizeof(float);
-    p.join_off = p.stat_off + slots * sizeof(float2);
-    p.bytes = p.join_off + (size_t)n_seq * max_new * n_heads * sizeof(uint2);
+    p.join_off = (p.stat_off + slots * sizeof(float2) + 15) & ~(size_t)15;
+    p.bytes = p.join_off + (size_t)n_seq * max_new * n_heads * sizeof(uint4);
     return p;
 }
 
@@ -707,11 +722,13 @@ hipError_t launch_kv8_attention(const Kv8Args& c, const uint16_t* q, int64_t q_s
     Kv8AttArgs a = {c, q, q_stride, row_start, pos0, n_seq, n_rows, max_new, rep, p.places, p.bound,
                     (float)(1.4426950408889634 / sqrt((double)c.head_dim)), out, static_cast<float*>(ws),
                     reinterpret_cast<float2*>(static_cast<uint8_t*>(ws) + p.stat_off),
-                    reinterpret_cast<uint2*>(static_cast<uint8_t*>(ws) + p.join_off)};
-    // row tiles that these rows can have
-    const uint64_t tiles = (uint64_t)n_rows * rep / (16 * p.nr) + (uint64_t)(n_seq < n_rows ? n_seq : n_rows);
-    const uint64_t most = (uint64_t)n_seq * p.tiles;
-    const dim3 grid((unsigned)((2 * p.places + (tiles < most ? tiles : most)) * c.n_kv));
+                    reinterpret_cast<uint4*>(static_cast<uint8_t*>(ws) + p.join_off)};
+    // Units that these rows can have (a workgroup that finds nothing to do is not free: a thousand of them are 3 us): their row tiles, each
+    // in no more stretches than the cache has spans; no more than run at once where stretches are made for that.
+    const uint64_t by_rows = (uint64_t)n_rows * rep / (16 * p.nr) + (uint64_t)(n_seq < n_rows ? n_seq : n_rows), by_seq = (uint64_t)n_seq * p.tiles;
+    const uint64_t tiles = by_rows < by_seq ? by_rows : by_seq, spans = (uint64_t)((c.max_pos + kAttSpan - 1) / kAttSpan);
+    const uint64_t most = 2 * tiles <= (uint64_t)p.places ? (uint64_t)p.places : 2 * (uint64_t)p.places + tiles;
+    const dim3 grid((unsigned)((tiles * spans < most ? tiles * spans : most) * c.n_kv));
     // (row, query head) pairs; few of them have many stretches each: four wavefronts
     const uint64_t pairs = (uint64_t)n_seq * max_new * n_heads;
     const bool wide = pairs <= 8u * (unsigned)device_cu_count();

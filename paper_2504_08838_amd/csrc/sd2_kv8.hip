@@ -3,6 +3,8 @@
 // A block of 32 positions of one head shares a scale, a power of two: a product with it is exact in fp32, bf16 and the matrix
 // instructions, so quantising rounds once, a block that is still open is brought to a larger scale by its exponents alone, and
 // attention applies scales where they cost nothing (keys: to the score; values: in the conversion to bf16).
+#include <algorithm>
+
 #include "sd2_internal.h"
 #include "sd2_rows.h"
 
@@ -702,7 +704,8 @@ Kv8Plan kv8_plan(int n_heads, int n_kv, int head_dim, int n_seq, int max_new) {
     p.dim = head_dim <= 64 ? 64 : head_dim <= 128 ? 128 : 256;
     p.nr = rows <= 16 || p.dim == 256 ? 1 : rows <= 32 || p.dim == 128 ? 2 : 4;
     const int kv = n_kv;
-    p.places = (2 * device_cu_count() + kv - 1) / kv;
+    const int by_lds = 163840 / kv8_lds(p.dim), by_registers = kv8_waves(p.dim, p.nr);
+    p.places = (std::min(by_lds, by_registers) * device_cu_count() + kv - 1) / kv;
     p.tiles = (rows + 16 * p.nr - 1) / (16 * p.nr);
     // units: sum of tiles * ceil(spans / stretch) <= sum of tiles * spans / stretch + sum of tiles
     p.bound = 2 * (uint32_t)p.places + (uint32_t)n_seq * (uint32_t)p.tiles;

@@ -20,10 +20,10 @@ namespace sd2 {
 // A workgroup is G groups of 32 rows times T teams: a team is a wavefront for each group, and the teams take turns with the tiles of
 // positions.  T teams take a T-th of the steps one after the other, and their results meet in LDS.  Where rows alone do not fill the chip,
 // what counts is the chain of steps.
-constexpr int prompt_tile(int dim, int g) { return g == 1 || dim == 256 ? 32 : 64; }
+constexpr int prompt_tile(int g) { return g == 1 ? 32 : 64; }
 // Keys and values of each team's tile.  Teams of several wavefronts have two buffers, as all of them must be through with one before it can
 // be filled again; a wavefront alone asks for its next keys when the scores are there and for its next values when these have been read.
-constexpr int prompt_tiles(int dim, int g, int t) { return t * (g == 1 ? 1 : 2) * 2 * prompt_tile(dim, g) * dim * 2; }
+constexpr int prompt_tiles(int dim, int g, int t) { return t * (g == 1 ? 1 : 2) * 2 * prompt_tile(g) * dim * 2; }
 constexpr int prompt_meeting(int dim, int g, int t) { return t > 1 ? t * 32 * g * (dim + 4 + 2) * 4 : 0; }  // rows of dim + 4 sums, maxima and sums of weights
 constexpr int prompt_lds(int dim, int g, int t) {
     return prompt_tiles(dim, g, t) > prompt_meeting(dim, g, t) ? prompt_tiles(dim, g, t) : prompt_meeting(dim, g, t);
@@ -61,8 +61,8 @@ __device__ __forceinline__ void load_to_lds(const void* base, uint32_t offset, u
 constexpr int wait_for(int n) { return 0x0F70 | (n & 15) | (n >> 4 << 14); }
 
 template <int D, int G, int T>
-__global__ __launch_bounds__(64 * G * T, G * T == 8 || D < 256 ? 2 : 1) void prompt_attention_kernel(PromptArgs a) {
-    constexpr int kTile = prompt_tile(D, G), kRb = kTile / 32, kSteps = D / 16, kDb = D / 32, kBytes = kTile * D * 2, kRows = 32 * G;
+__global__ __launch_bounds__(64 * G * T, D < 256 ? 2 : 1) void prompt_attention_kernel(PromptArgs a) {
+    constexpr int kTile = prompt_tile(G), kRb = kTile / 32, kSteps = D / 16, kDb = D / 32, kBytes = kTile * D * 2, kRows = 32 * G;
     constexpr int kCalls = kBytes / (1024 * G);  // requests of a wavefront for a tile of keys (and of values)
     constexpr int kAhead = kTile * T;            // positions from a team's tile to its next
     extern __shared__ __attribute__((aligned(16))) uint8_t whole[];  // [team][kBuffers][keys, values][kBytes]
@@ -376,8 +376,7 @@ hipError_t launch_prompt_attention(const uint16_t* q, const uint16_t* k, const u
     else if (head_dim <= 128 && few) SD2_PROMPT(128, 1, 4);
     else if (head_dim <= 128 && some) SD2_PROMPT(128, 4, 2);
     else if (head_dim <= 128) SD2_PROMPT(128, 4, 1);
-    else if (few) SD2_PROMPT(256, 1, 4);
-    else SD2_PROMPT(256, 4, 1);
+    else SD2_PROMPT(256, 1, 4);  // one tile of 128 rows leaves the registers no room for a second wavefront (6000 tokens: 256 / 281 us)
 #undef SD2_PROMPT
     return hipGetLastError();
 }

@@ -80,20 +80,32 @@ def attention(q: np.ndarray, k: np.ndarray, v: np.ndarray, reach) -> np.ndarray:
     bounds, the weighted magnitudes sum_j w_j |v_j| and the largest sum of |q_d k_d| of a row."""
     rows, n_heads, dim = q.shape
     rep = n_heads // k.shape[0]
+    reach = np.minimum(np.asarray(reach), k.shape[1] - 1)
     out, mass, dot = np.zeros_like(q), np.zeros_like(q), np.zeros((rows, n_heads))
-    with np.errstate(invalid="ignore", over="ignore"):  # infinities and NaN go their way
-        for i in range(rows):
-            n = min(int(reach[i]) + 1, k.shape[1])
-            if n <= 0:
-                continue
-            for h in range(n_heads):
-                kk, vv = k[h // rep, :n], v[h // rep, :n]
-                s = kk @ q[i, h] / np.sqrt(float(dim))
+    some = np.flatnonzero(reach >= 0)
+    if not some.size:
+        return out, mass, dot
+    last = int(reach.max()) + 1
+    finite = all(np.isfinite(x).all() for x in (q, k[:, :last], v[:, :last]))
+    for h in range(n_heads):
+        kk, vv = k[h // rep, :last], v[h // rep, :last]
+        if finite:  # all rows at once: a weight of zero for what a row does not attend to
+            off = np.arange(last)[None, :] > reach[some, None]
+            s = np.where(off, -np.inf, q[some, h] @ kk.T / np.sqrt(float(dim)))
+            e = np.exp(s - s.max(axis=1, keepdims=True))
+            w = e / e.sum(axis=1, keepdims=True)
+            out[some, h], mass[some, h] = w @ vv, w @ np.abs(vv)
+            dot[some, h] = np.where(off, 0.0, np.abs(q[some, h]) @ np.abs(kk).T).max(axis=1) / np.sqrt(float(dim))
+            continue
+        with np.errstate(invalid="ignore", over="ignore"):  # infinities and NaN go their way: only what a row attends to enters
+            for i in some:
+                n = int(reach[i]) + 1
+                s = kk[:n] @ q[i, h] / np.sqrt(float(dim))
                 e = np.exp(s - s.max())
                 w = e / e.sum()
-                out[i, h] = w @ vv
-                mass[i, h] = w @ np.abs(vv)
-                dot[i, h] = (np.abs(kk) @ np.abs(q[i, h])).max() / np.sqrt(float(dim))
+                out[i, h] = w @ vv[:n]
+                mass[i, h] = w @ np.abs(vv[:n])
+                dot[i, h] = (np.abs(kk[:n]) @ np.abs(q[i, h])).max() / np.sqrt(float(dim))
     return out, mass, dot
 
 

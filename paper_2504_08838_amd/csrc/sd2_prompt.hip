@@ -57,8 +57,18 @@ __device__ __forceinline__ void load_to_lds(const void* base, uint32_t offset, u
     asm volatile("s_mov_b32 m0, %2\n\ts_nop 0\n\tglobal_load_lds_dwordx4 %0, %1" ::"v"(offset), "s"(base), "s"(lds) : "memory");
 }
 
-// the wait for all but the last n vector memory operations
-constexpr int wait_for(int n) { return 0x0F70 | (n & 15) | (n >> 4 << 14); }
+// Waits for all but the last N vector memory operations, and for all operations on LDS; nothing moves across them.
+template <int N>
+__device__ __forceinline__ void wait_memory() {
+    asm volatile("" ::: "memory");
+    __builtin_amdgcn_s_waitcnt(0x0F70 | (N & 15) | (N >> 4 << 14));
+    asm volatile("" ::: "memory");
+}
+__device__ __forceinline__ void wait_lds() {
+    asm volatile("" ::: "memory");
+    __builtin_amdgcn_s_waitcnt(0xC07F);
+    asm volatile("" ::: "memory");
+}
 
 template <int D, int G, int T>
 __global__ __launch_bounds__(64 * G * T, D < 256 ? 2 : 1) void prompt_attention_kernel(PromptArgs a) {
@@ -162,6 +172,7 @@ __global__ __launch_bounds__(64 * G * T, D < 256 ? 2 : 1) void prompt_attention_
                 const bf16x8 kf = *reinterpret_cast<const bf16x8*>(kt + key_place<D>(32 * rb + key_row, 2 * i + h));
                 s[rb] = __builtin_amdgcn_mfma_f32_32x32x16_bf16(kf, q[i], s[rb], 0, 0, 0);
             }
+        // six reads of LDS under way in front of each product (8192 tokens: 399 us; as the compiler orders them, two: 409)
         __builtin_amdgcn_sched_group_barrier(0x100, 6, 0);
 #pragma unroll
         for (int i = 0; i < kSteps * kRb; ++i) {
@@ -170,8 +181,7 @@ __global__ __launch_bounds__(64 * G * T, D < 256 ? 2 : 1) void prompt_attention_
         }
         if constexpr (G == 1) {
             if (base + kAhead < n_pos) {
-                __builtin_amdgcn_s_waitcnt(0xC07F);  // the keys have been read
-                asm volatile("" ::: "memory");
+                wait_lds();  // the keys have been read
                 request(base + kAhead, 0, Keys());
             }
         }
@@ -197,9 +207,8 @@ __global__ __launch_bounds__(64 * G * T, D < 256 ? 2 : 1) void prompt_attention_
             for (int d = 0; d < kDb; ++d) o[d] *= f;
         }
         if constexpr (G == 1) {  // this tile's values: all but the keys just asked for
-            if (base + kAhead < n_pos) __builtin_amdgcn_s_waitcnt(wait_for(kCalls));
-            else __builtin_amdgcn_s_waitcnt(wait_for(0));
-            asm volatile("" ::: "memory");
+            if (base + kAhead < n_pos) wait_memory<kCalls>();
+            else wait_memory<0>();
         }
         if (masked) {
             // A weight of zero times an infinity or NaN is NaN, also where the row does not attend to the position: from the first tile
@@ -246,25 +255,22 @@ __global__ __launch_bounds__(64 * G * T, D < 256 ? 2 : 1) void prompt_attention_
         l += sum[0] + sum[1];
         if constexpr (G == 1) {
             if (base + kAhead < n_pos) {
-                __builtin_amdgcn_s_waitcnt(0xC07F);  // the values have been read
-                asm volatile("" ::: "memory");
+                wait_lds();  // the values have been read
                 request(base + kAhead, 0, Values());
             }
         }
     };
     auto next = [&]() __attribute__((always_inline)) {
         if constexpr (G == 1) {
-            __builtin_amdgcn_s_waitcnt(wait_for(kCalls));  // the keys: all but the values behind them
-            asm volatile("" ::: "memory");
+            wait_memory<kCalls>();  // the keys: all but the values behind them
         } else {
-            __builtin_amdgcn_s_waitcnt(wait_for(0));  // this wavefront's requests
-            asm volatile("" ::: "memory");
+            wait_memory<0>();  // this wavefront's requests
             __syncthreads();  // everybody's: the tile is there, and nobody reads the other buffer
             if (base + kAhead < n_pos) request(base + kAhead, buf ^ 1, Both());
         }
     };
     // the queries with the first tile: a wait of the compiler's for them would be one for what is asked for behind them as well
-    if (G == 1) __builtin_amdgcn_s_waitcnt(wait_for(0));
+    if (G == 1) wait_memory<0>();
     const int last = n_pos + kTile * team;           // as many steps for every team
     for (; base < last && base + kTile - 1 <= wave_low; base += kAhead, buf ^= kBuffers - 1) {  // all rows attend to all positions
         next();

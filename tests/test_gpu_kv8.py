@@ -232,6 +232,47 @@ def test_attention_many_sequences():
     check_attention(attend(slots, q, 2, lens, pos0, n_rows=sum(lens)), q, k, v, 2, lens, pos0, 64)
 
 
+@pytest.mark.parametrize("n_heads,n_kv,dim", [(16, 8, 64), (24, 8, 128), (8, 4, 256), (24, 8, 96)])
+def test_attention_more_row_tiles_than_places(n_heads, n_kv, dim):
+    """So many sequences that whole stretches go first and what is left of each follows; some idle, some of one position."""
+    n_seq = 160
+    rng = np.random.default_rng(22)
+    lens = rng.choice([0, 1, 1, 2, 5], n_seq).tolist()
+    pos0 = (rng.random(n_seq) ** 3 * 1400).astype(int).tolist()
+    slots, q, k, v = filled(lens, pos0, n_heads, n_kv, dim, 1440)
+    check_attention(attend(slots, q, n_heads, lens, pos0, n_rows=sum(lens)), q, k, v, n_heads, lens, pos0, dim)
+
+
+def test_attention_of_stretches_of_many_tiles():
+    """So many heads that a stretch is longer than what a wavefront holds scales for; three heads against the oracle."""
+    n_kv, dim, max_pos, lens, pos0 = 512, 16, 33 * 1024, [2, 1], [33 * 1024 - 2, 20011]
+    gen = torch.Generator(device="cuda")
+    gen.manual_seed(23)
+    slots = Slots(2, n_kv, max_pos, dim)
+    for c in (slots.k, slots.v):
+        c.copy_((torch.randn(c.shape, generator=gen, device="cuda") * 95).clamp_(-448, 448).to(torch.float8_e4m3fn).view(torch.uint8))
+    for c in (slots.ks, slots.vs):
+        c.copy_(torch.exp2(torch.randint(-9, -5, c.shape, generator=gen, device="cuda").float()))
+    q = torch.randn(3, n_kv * dim, generator=torch.Generator().manual_seed(24)).to(torch.bfloat16).cuda()
+    got = f64(attend(slots, q, n_kv, lens, pos0)).reshape(3, n_kv, dim)
+    for h in (0, 77, 511):
+        for b, rows in ((0, slice(0, 2)), (1, slice(2, 3))):
+            k, v = (kv8.values(c[b, h:h + 1].cpu().numpy(), s[b, h:h + 1].cpu().numpy()) for c, s in ((slots.k, slots.ks), (slots.v, slots.vs)))
+            want, mass, dot = kv8.attention(f64(q).reshape(3, n_kv, dim)[rows, h:h + 1], k, v, pos0[b] + np.arange(lens[b]))
+            assert (np.abs(got[rows, h:h + 1] - want) <= bound(want, mass, dot, dim)).all()
+
+
+@pytest.mark.parametrize("n_heads,n_kv,dim", [(4, 2, 64), (24, 8, 128), (8, 2, 256)])
+def test_same_bits_every_time(n_heads, n_kv, dim):
+    """Over and over, other values in between: what a buffer of LDS or the workspace holds from before never shows."""
+    lens, pos0 = [5, 1, 17], [900, 3000, 130]
+    slots, q, _, _ = filled(lens, pos0, n_heads, n_kv, dim, 3072)
+    first = attend(slots, q, n_heads, lens, pos0, n_rows=23).view(torch.int16)
+    for _ in range(20):
+        attend(slots, q * 20, n_heads, [3, 20], [2500, 1000], n_rows=23)
+        assert torch.equal(attend(slots, q, n_heads, lens, pos0, n_rows=23).view(torch.int16), first)
+
+
 def test_attention_of_the_first_rows_only():
     lens, pos0 = [7, 5], [50, 60]
     slots, q, k, v = filled(lens, pos0, 4, 2, 64, 96)

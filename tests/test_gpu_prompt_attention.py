@@ -188,3 +188,64 @@ def test_offsets_that_break_the_rules_stay_inside_the_buffers():
     sd2.prompt_attention(q.data_ptr(), k.data_ptr(), v.data_ptr(), 128, 64, rs.data_ptr(), 5, 50, 2, 1, 64, out.data_ptr(), gu.stream_ptr())
     torch.cuda.synchronize()
     assert (out[50:] == 7.0).all()
+
+
+# Which kernel a call gets goes by its rows times query heads of a group: what is above gets the one for few.  SOME (4500 and 6000 of them
+# for each key/value head) gets the one with two teams, MANY (12000 and 16000) the one of the longest calls; prompts of all lengths in both.
+SOME = [300, 1, 0, 129, 640, 64, 33, 2, 331]
+MANY = [40 + 7 * i for i in range(24)] + [0, 1, 65, 700, 128, 250]
+WIDE = [(24, 8, 128), (32, 8, 64), (24, 8, 80), (32, 8, 48)]
+
+
+@pytest.mark.parametrize("n_heads,n_kv,dim", WIDE)
+@pytest.mark.parametrize("lens", [SOME, MANY], ids=["some", "many"])
+def test_more_rows_than_the_chip_takes_at_once(n_heads, n_kv, dim, lens):
+    n = sum(lens)
+    q, k, v = rows(50, n, n_heads, dim), rows(51, n, n_kv, dim), rows(52, n, n_kv, dim)
+    check(run(q, k, v, lens, n_heads, n_kv, dim), q, k, v, lens, n_heads, n_kv, dim)
+
+
+@pytest.mark.parametrize("n_heads,n_kv,dim", WIDE[:3])
+@pytest.mark.parametrize("lens", [SOME, MANY], ids=["some", "many"])
+def test_more_rows_with_values_that_are_not_finite(n_heads, n_kv, dim, lens):
+    """One prompt's values hold NaN and infinities; the others' results stay as they are, and its own rows get what they attend to."""
+    n, b = sum(lens), lens.index(640 if 640 in lens else 700)
+    at = starts(lens)[b]
+    q, k, v = rows(53, n, n_heads, dim), rows(54, n, n_kv, dim), rows(55, n, n_kv, dim)
+    clean = run(q, k, v, lens, n_heads, n_kv, dim)
+    v[at + 70, 3], v[at + 200, dim], v[at + 333, dim - 1] = float("nan"), float("inf"), float("-inf")
+    out = run(q, k, v, lens, n_heads, n_kv, dim)
+    part, m = slice(at, at + lens[b]), lens[b]
+    check(out[part], q[part], k[part], v[part], [m], n_heads, n_kv, dim)
+    outside = torch.ones(n, dtype=torch.bool)
+    outside[part] = False
+    assert torch.equal(out[outside.cuda()].view(torch.int16), clean[outside.cuda()].view(torch.int16))
+
+
+@pytest.mark.parametrize("lens", [SOME, MANY], ids=["some", "many"])
+def test_more_rows_inside_longer_ones_and_rows_behind_the_last_sequence(lens):
+    n, dim = sum(lens) + 5, 128
+    q, k, v = rows(56, n, 24, dim, 24 * dim + 64), rows(57, n, 8, dim, 8 * dim + 8), rows(58, n, 8, dim, 8 * dim + 8)
+    for t in (q, k, v):
+        t[sum(lens):] = float("nan")
+    check(run(q, k, v, lens, 24, 8, dim), q, k, v, lens, 24, 8, dim)
+
+
+def test_a_long_prompt_of_the_largest_kernel_row_by_row():
+    n, n_heads, n_kv, dim = 5000, 24, 8, 128
+    q, k, v = rows(59, n, n_heads, dim), rows(60, n, n_kv, dim), rows(61, n, n_kv, dim)
+    out = f64(run(q, k, v, [n], n_heads, n_kv, dim)).reshape(n, n_heads, dim)
+    pick = [0, 1, 41, 42, 43, 63, 64, 127, 128, 2047, 2048, 4095, 4096, 4998, 4999]
+    want, mass, dot = kv8.attention(split(q, n_heads, dim)[pick], split(k, n_kv, dim).transpose(1, 0, 2), split(v, n_kv, dim).transpose(1, 0, 2), pick)
+    assert (np.abs(out[pick] - want) <= bound(want, mass, dot, dim)).all()
+
+
+@pytest.mark.parametrize("n,repeats", [(500, 20), (1500, 20), (4000, 10)])
+def test_same_bits_every_time(n, repeats):
+    """Each kernel, over and over on other values in between: what a buffer of LDS holds from before never shows."""
+    q, k, v = rows(62, n, 24, 128), rows(63, n, 8, 128), rows(64, n, 8, 128)
+    other = [rows(65 + i, n, h, 128) * 30 for i, h in enumerate((24, 8, 8))]
+    first = run(q, k, v, [n], 24, 8, 128).view(torch.int16)
+    for _ in range(repeats):
+        run(*other, [n], 24, 8, 128)
+        assert torch.equal(run(q, k, v, [n], 24, 8, 128).view(torch.int16), first)

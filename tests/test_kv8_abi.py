@@ -75,6 +75,10 @@ def test_cached_attention_workspace():
     assert 0 < small <= large
     for args, status in (((3, 1, 1), SHAPE), ((4, 5, 1), RANGE), ((4, -1, 1), RANGE), ((4, 1, 0), RANGE), ((4, 1, 65), RANGE)):
         assert _status(sd2.kv8_attention_workspace_size, c, *args) == status
+    large = _cache(n_slots=65536, n_kv=1)
+    assert sd2.kv8_attention_workspace_size(large, 64, 65536, 64) > 0
+    many = _cache(n_slots=65536, n_kv=4096)
+    assert _status(sd2.kv8_attention_workspace_size, many, 4096, 65536, 64) == RANGE  # more than 2^30 rows of heads
     assert sd2.lib().sd2_kv8_attention_workspace_size(C.byref(c), 4, 1, 1, None) == NULL
     assert sd2.lib().sd2_kv8_attention_workspace_size(None, 4, 1, 1, C.byref(C.c_size_t())) == NULL
 

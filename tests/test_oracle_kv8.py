@@ -65,3 +65,14 @@ def test_prompt_attention_by_loops():
     s = np.array([q[5, 3] @ k[j, 1] for j in (3, 4, 5)]) / np.sqrt(8.0)
     w = np.exp(s) / np.exp(s).sum()
     assert np.allclose(out[5, 3], w @ v[3:6, 1])
+
+
+def test_attention_all_rows_at_once_is_row_by_row():
+    rng = np.random.default_rng(9)
+    q, k, v = rng.standard_normal((5, 4, 8)), rng.standard_normal((2, 9, 8)), rng.standard_normal((2, 9, 8))
+    reach = [3, -1, 0, 20, 5]
+    odd = v.copy()
+    odd[:, 7] = np.nan  # a position that only the fourth row attends to: the others' results are those without it
+    for whole, single in zip(kv8.attention(q, k, v, reach), kv8.attention(q, k, odd, reach)):
+        assert np.allclose(np.delete(whole, 3, axis=0), np.delete(single, 3, axis=0), rtol=1e-13, atol=1e-13)
+    assert np.isnan(kv8.attention(q, k, odd, reach)[0][3]).all()

@@ -320,7 +320,11 @@ __device__ __forceinline__ void read_values(i32x2 (&v)[N], const uint32_t (&at)[
             : "memory");
 }
 
-constexpr int kv8_lds(int dim) { return kAttWaves * 2 * 2 * 32 * dim; }
+// the wavefronts' tiles, and afterwards their results: rows of dim + 4 sums, maxima and sums of weights
+constexpr int kv8_lds(int dim, int nr) {
+    const int tiles = kAttWaves * 2 * 2 * 32 * dim, results = kAttWaves * 16 * nr * (dim + 4 + 2) * 4;
+    return tiles > results ? tiles : results;
+}
 // wavefronts that share a SIMD's registers
 constexpr int kv8_waves(int dim, int nr) { return dim == 256 ? 1 : dim * nr <= 64 ? 4 : dim * nr <= 128 ? 3 : 2; }
 
@@ -328,7 +332,6 @@ template <int D, int NR>
 __global__ __launch_bounds__(64 * kAttWaves, kv8_waves(D, NR)) void kv8_attention_kernel(Kv8AttArgs a) {
     constexpr int kRows = 16 * NR, kDb = D / 16, kJ = D / 64, kPieces = D / 16, kTile = 32 * D, kLoads = kTile / 1024;
     constexpr int kORow = D + 4;  // floats
-    static_assert(kAttWaves * (16 * kORow + 32) * 4 <= kv8_lds(D), "the wavefronts' results fit where the tiles were");
     extern __shared__ __attribute__((aligned(16))) uint8_t smem[];  // [wave][buffer][keys, values][32][D]
     const int tid = threadIdx.x, lane = tid & 63, wave = __builtin_amdgcn_readfirstlane(tid >> 6), n = lane & 15, g = lane >> 4;
     const int grp = blockIdx.x % a.c.n_kv;
@@ -481,13 +484,14 @@ __global__ __launch_bounds__(64 * kAttWaves, kv8_waves(D, NR)) void kv8_attentio
             zero.q = u32x4{0, 0, 0, 0};
             p[t] = zero.v;
             if (t && 16 * t >= rows_here) continue;
-            float w[8], mx = -3.0e38f;
+            float w[8], mx = -__builtin_inff();
 #pragma unroll
             for (int e = 0; e < 8; ++e) {
-                w[e] = s[t][e >> 2][e & 3] * c;
+                w[e] = s[t][e >> 2][e & 3];
                 if (masked && base + 8 * g + e > reach[t]) w[e] = -__builtin_inff();
                 mx = fmaxf(mx, w[e]);
             }
+            mx = fmaxf(mx * c, -3.0e38f);
             // The maximum follows only where a weight could grow past 2^8: sums of weights up to that are as exact as those below 1.
             if (__any(mx > m[t] + 8.f)) {
                 const float top = fmaxf(m[t], max_quarters(max_halves(mx))), f = __builtin_amdgcn_exp2f(m[t] - top);
@@ -499,7 +503,7 @@ __global__ __launch_bounds__(64 * kAttWaves, kv8_waves(D, NR)) void kv8_attentio
             Frag pair;
 #pragma unroll
             for (int e = 0; e < 8; ++e) {
-                w[e] = __builtin_amdgcn_exp2f(w[e] - m[t]);
+                w[e] = __builtin_amdgcn_exp2f(__builtin_fmaf(w[e], c, -m[t]));
                 l[t] += w[e];
             }
 #pragma unroll
@@ -557,33 +561,37 @@ __global__ __launch_bounds__(64 * kAttWaves, kv8_waves(D, NR)) void kv8_attentio
         }
     }
 
-    // the wavefronts' results meet in LDS, sixteen rows at a time
-    float* mo = reinterpret_cast<float*>(smem);                     // [wave][16][kORow]
-    float2* mstat = reinterpret_cast<float2*>(mo + kAttWaves * 16 * kORow);  // [wave][16]
+    // the wavefronts' results meet in LDS
+    float* mo = reinterpret_cast<float*>(smem);                                  // [wave][kRows][kORow]
+    float2* mstat = reinterpret_cast<float2*>(mo + kAttWaves * kRows * kORow);  // [wave][kRows]
+    __syncthreads();
 #pragma unroll
     for (int t = 0; t < NR; ++t) {
         if (t && 16 * t >= rows_here) break;
+        const int at = kRows * wave + 16 * t + n;
         const float sum = sum_quarters(sum_halves(l[t]));
-        __syncthreads();
 #pragma unroll
-        for (int d = 0; d < kDb; ++d) *reinterpret_cast<f32x4*>(mo + (16 * wave + n) * kORow + 16 * d + 4 * g) = o[t][d];
-        if (g == 0) mstat[16 * wave + n] = make_float2(m[t], sum);
-        __syncthreads();
-        const int r16 = tid >> 4, row = first + 16 * t + r16;  // sixteen threads a row
+        for (int d = 0; d < kDb; ++d) *reinterpret_cast<f32x4*>(mo + at * kORow + 16 * d + 4 * g) = o[t][d];
+        if (g == 0) mstat[at] = make_float2(m[t], sum);
+    }
+    __syncthreads();
+#pragma unroll
+    for (int t = 0; t < NR; ++t) {
+        const int mine = 16 * t + (tid >> 4), row = first + mine;  // sixteen threads a row
         if (row < n_used) {
             float w[kAttWaves], top = -3.0e38f, all = 0.f;
 #pragma unroll
-            for (int i = 0; i < kAttWaves; ++i) top = fmaxf(top, mstat[16 * i + r16].x);
+            for (int i = 0; i < kAttWaves; ++i) top = fmaxf(top, mstat[kRows * i + mine].x);
 #pragma unroll
             for (int i = 0; i < kAttWaves; ++i) {
-                const float2 st = mstat[16 * i + r16];
+                const float2 st = mstat[kRows * i + mine];
                 w[i] = __builtin_amdgcn_exp2f(st.x - top);
                 all += w[i] * st.y;
             }
             const int token = row / rep;
             // a row that attends to nothing is zero
             const float inv = pos0 + token < 0 ? 0.f : 1.0f / all;
-            const size_t slot = ((size_t)unit * a.c.n_kv + grp) * kRows + 16 * t + r16;
+            const size_t slot = ((size_t)unit * a.c.n_kv + grp) * kRows + mine;
             if ((tid & 15) == 0) {
                 if (cuts > 1) a.stat[slot] = make_float2(top, all);
                 uint4* join = a.join + ((size_t)u.seq * a.max_new + token) * (a.c.n_kv * rep) + grp * rep + (row - token * rep);
@@ -595,7 +603,7 @@ __global__ __launch_bounds__(64 * kAttWaves, kv8_waves(D, NR)) void kv8_attentio
                 if (d >= D_used) break;
                 f32x4 x = f32x4{0.f, 0.f, 0.f, 0.f};
 #pragma unroll
-                for (int i = 0; i < kAttWaves; ++i) x += *reinterpret_cast<const f32x4*>(mo + (16 * i + r16) * kORow + d) * w[i];
+                for (int i = 0; i < kAttWaves; ++i) x += *reinterpret_cast<const f32x4*>(mo + (kRows * i + mine) * kORow + d) * w[i];
                 if (cuts > 1) {
                     *reinterpret_cast<f32x4*>(a.part + slot * D + d) = x;
                 } else {
@@ -704,7 +712,7 @@ Kv8Plan kv8_plan(int n_heads, int n_kv, int head_dim, int n_seq, int max_new) {
     p.dim = head_dim <= 64 ? 64 : head_dim <= 128 ? 128 : 256;
     p.nr = rows <= 16 || p.dim == 256 ? 1 : rows <= 32 || p.dim == 128 ? 2 : 4;
     const int kv = n_kv;
-    const int by_lds = 163840 / kv8_lds(p.dim), by_registers = kv8_waves(p.dim, p.nr);
+    const int by_lds = 163840 / kv8_lds(p.dim, p.nr), by_registers = kv8_waves(p.dim, p.nr);
     p.places = (std::min(by_lds, by_registers) * device_cu_count() + kv - 1) / kv;
     p.tiles = (rows + 16 * p.nr - 1) / (16 * p.nr);
     // units: sum of tiles * ceil(spans / stretch) <= sum of tiles * spans / stretch + sum of tiles
@@ -739,9 +747,9 @@ hipError_t launch_kv8_attention(const Kv8Args& c, const uint16_t* q, int64_t q_s
 #define SD2_KV8(DIM, R)                                                                                                   \
     if (p.dim == DIM && p.nr == R) {                                                                                      \
         static std::atomic<uint64_t> done{0};                                                                             \
-        const hipError_t e = allow_lds(reinterpret_cast<const void*>(&kv8_attention_kernel<DIM, R>), kv8_lds(DIM), done); \
+        const hipError_t e = allow_lds(reinterpret_cast<const void*>(&kv8_attention_kernel<DIM, R>), kv8_lds(DIM, R), done); \
         if (e != hipSuccess) return e;                                                                                    \
-        hipLaunchKernelGGL((kv8_attention_kernel<DIM, R>), grid, dim3(64 * kAttWaves), kv8_lds(DIM), s, a);               \
+        hipLaunchKernelGGL((kv8_attention_kernel<DIM, R>), grid, dim3(64 * kAttWaves), kv8_lds(DIM, R), s, a);               \
         if (c.max_pos > kAttSpan && wide) hipLaunchKernelGGL((kv8_combine_kernel<DIM, R, 4>), join, dim3(256), 0, s, a);  \
         if (c.max_pos > kAttSpan && !wide) hipLaunchKernelGGL((kv8_combine_kernel<DIM, R, 1>), join, dim3(256), 0, s, a); \
     }

@@ -95,7 +95,8 @@ __global__ __launch_bounds__(64 * G * T, D < 256 ? 2 : 1) void prompt_attention_
     uint8_t* smem = whole + team * kBuffers * 2 * kBytes;
     const int first = kRows * (int)u.index, wave_first = first + 32 * member;
     const int n_pos = min(first + kRows - 1, n_used - 1) / rep + 1;               // positions that the workgroup's rows attend to
-    const int wave_pos = wave_first < n_used ? min(wave_first + 31, n_used - 1) / rep + 1 : 0, wave_low = wave_first / rep;
+    // of the wavefront's own rows: positions that the last attends to, and the last position that all attend to (no rows: none)
+    const int wave_pos = wave_first < n_used ? min(wave_first + 31, n_used - 1) / rep + 1 : 0, wave_low = wave_first < n_used ? wave_first / rep : -1;
     const uint16_t* kg = a.k + (size_t)sr.start * a.kv_stride + (size_t)grp * hd;
     const uint16_t* vg = a.v + (size_t)sr.start * a.kv_stride + (size_t)grp * hd;
 

@@ -266,7 +266,7 @@ def test_attention_of_stretches_of_many_tiles():
 def test_same_bits_every_time(n_heads, n_kv, dim):
     """Over and over, other values in between: what a buffer of LDS or the workspace holds from before never shows."""
     lens, pos0 = [5, 1, 17], [900, 3000, 130]
-    slots, q, _, _ = filled(lens, pos0, n_heads, n_kv, dim, 3072)
+    slots, q, _, _ = filled(lens, pos0, n_heads, n_kv, dim, 3104)
     first = attend(slots, q, n_heads, lens, pos0, n_rows=23).view(torch.int16)
     for _ in range(20):
         attend(slots, q * 20, n_heads, [3, 20], [2500, 1000], n_rows=23)

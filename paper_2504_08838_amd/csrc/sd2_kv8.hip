@@ -214,7 +214,7 @@ hipError_t launch_kv8_append(const Kv8Args& c, const float* qkv, int n_heads, co
 //
 // The rows of a workgroup are (token, query head of the group) pairs in that order, up to 16 NR of them, so that a cached position
 // is read and converted once for all of them.  A workgroup takes a stretch of positions, its four wavefronts every fourth tile of
-// 32 -- one block, so a tile has one scale.  Scores come out transposed (positions by rows): a lane then holds eight positions of one
+// 32 -- one block, so a tile has one scale; short caches are not cut, and eight wavefronts take all of one.  Scores come out transposed (positions by rows): a lane then holds eight positions of one
 // row, which is how the next product wants its operand, so weights never leave the registers.  Positions are dealt to the rows of the
 // first product such that those eight follow one another.  Tiles go from memory straight into LDS, one ahead of the one at work, and values
 // leave it by the transposing read.  Weights are rounded to bf16 for the second product, at most 2^-8 of a weight.
@@ -223,8 +223,8 @@ hipError_t launch_kv8_append(const Kv8Args& c, const float* qkv, int n_heads, co
 // 4.9 TB/s, where a pure read has 5.35 (and 5 us to join); by the chain plan - first tile - scores - meeting - join where there are few: one token against 429
 // positions 8.3 us, five against 30016 15 us.  64 tokens with four query heads a group: 1.9 us for 128 positions of 64 rows, softmax and
 // conversions on the vector ALU.
-constexpr int kAttWaves = 4;
-constexpr int kAttSpan = 32 * kAttWaves;  // positions of the workgroup's tiles side by side
+constexpr int kCutWaves = 4, kWholeWaves = 8;  // wavefronts of a workgroup that takes a stretch, and of one that takes all positions
+constexpr int kAttSpan = 32 * kCutWaves;        // positions of four tiles side by side: what stretches are made of
 
 constexpr uint32_t kRest = 0x80000000u;
 
@@ -329,15 +329,16 @@ __device__ __forceinline__ void read_values(i32x2 (&v)[N], const uint32_t (&at)[
 }
 
 // the wavefronts' tiles, and afterwards their results: rows of dim + 4 sums, maxima and sums of weights
-constexpr int kv8_lds(int dim, int nr) {
-    const int tiles = kAttWaves * 2 * 2 * 32 * dim, results = kAttWaves * 16 * nr * (dim + 4 + 2) * 4;
+constexpr int kv8_lds(int dim, int nr, int waves) {
+    const int tiles = waves * 2 * 2 * 32 * dim, results = waves * 16 * nr * (dim + 4 + 2) * 4;
     return tiles > results ? tiles : results;
 }
 // wavefronts that share a SIMD's registers
-constexpr int kv8_waves(int dim, int nr) { return dim == 256 ? 1 : dim * nr <= 64 ? 4 : dim * nr <= 128 ? 3 : 2; }
+constexpr int kv8_waves(int dim, int nr, int waves) { return waves == kWholeWaves ? 2 : dim == 256 ? 1 : dim * nr <= 64 ? 4 : dim * nr <= 128 ? 3 : 2; }
 
-template <int D, int NR>
-__global__ __launch_bounds__(64 * kAttWaves, kv8_waves(D, NR)) void kv8_attention_kernel(Kv8AttArgs a) {
+// W: kCutWaves or kWholeWaves
+template <int D, int NR, int W>
+__global__ __launch_bounds__(64 * W, kv8_waves(D, NR, W)) void kv8_attention_kernel(Kv8AttArgs a) {
     constexpr int kRows = 16 * NR, kDb = D / 16, kJ = D / 64, kPieces = D / 16, kTile = 32 * D, kLoads = kTile / 1024;
     constexpr int kORow = D + 4;  // floats
     extern __shared__ __attribute__((aligned(16))) uint8_t smem[];  // [wave][buffer][keys, values][32][D]
@@ -345,18 +346,24 @@ __global__ __launch_bounds__(64 * kAttWaves, kv8_waves(D, NR)) void kv8_attentio
     const int grp = blockIdx.x % a.c.n_kv;
     const uint32_t unit = blockIdx.x / a.c.n_kv;
     const Sequences seqs(a.row_start, a.pos0, a.n_seq, a.n_rows);
-    bool many;
-    const uint32_t stretch = stretch_of<kRows>(a, seqs, many);
-    // with many, whole stretches first, then what is left of each sequence
-    auto whole = [&](const SeqRows& r) {
-        const SeqCut s = seq_cut<kRows>(a, r);
-        return s.tiles * ((many ? s.spans : s.spans + stretch - 1) / stretch);
-    };
-    const uint32_t n_whole = many ? (uint32_t)seqs.total(whole) : ~0u;
-    const SeqUnit u = unit < n_whole ? seqs.find(unit, whole) : seqs.find(unit - n_whole, [&](const SeqRows& r) {
-        const SeqCut s = seq_cut<kRows>(a, r);
-        return s.spans % stretch ? s.tiles : 0u;
-    });
+    bool many = false;
+    uint32_t stretch = 1u << 13, n_whole = ~0u;  // as many spans as the longest cache has
+    SeqUnit u;
+    if constexpr (W == kWholeWaves) {
+        u = seqs.find(unit, [&](const SeqRows& r) { return seq_cut<kRows>(a, r).tiles; });
+    } else {
+        stretch = stretch_of<kRows>(a, seqs, many);
+        // with many, whole stretches first, then what is left of each sequence
+        auto whole = [&](const SeqRows& r) {
+            const SeqCut s = seq_cut<kRows>(a, r);
+            return s.tiles * ((many ? s.spans : s.spans + stretch - 1) / stretch);
+        };
+        if (many) n_whole = (uint32_t)seqs.total(whole);
+        u = unit < n_whole ? seqs.find(unit, whole) : seqs.find(unit - n_whole, [&](const SeqRows& r) {
+            const SeqCut s = seq_cut<kRows>(a, r);
+            return s.spans % stretch ? s.tiles : 0u;
+        });
+    }
     if (u.seq < 0) return;
     const SeqCut sc = seq_cut<kRows>(a, u.rows);
     const int64_t pos0 = u.rows.pos0;
@@ -442,14 +449,14 @@ __global__ __launch_bounds__(64 * kAttWaves, kv8_waves(D, NR)) void kv8_attentio
     // Waits for vector memory are written out: one that the compiler puts where a value is used would be one for the requests as well.
     float k_scales = 0.f, v_scales = 0.f;  // of the wavefront's next 64 tiles, one in each lane
     auto load_scales = [&]() __attribute__((always_inline)) {
-        const int block = min(base / kBlock + kAttWaves * lane, a.c.max_pos / kBlock - 1);
+        const int block = min(base / kBlock + W * lane, a.c.max_pos / kBlock - 1);
         k_scales = ks[block];
         v_scales = vs[block];
     };
     if (base < to) load_scales();
     __builtin_amdgcn_s_waitcnt(0x0F70);  // the scales, the queries and the first tile
     asm volatile("" : "+v"(k_scales), "+v"(v_scales)::"memory");
-    for (int buf = 0, i = 0; base < to; base += kAttSpan, buf ^= 1, ++i) {
+    for (int buf = 0, i = 0; base < to; base += 32 * W, buf ^= 1, ++i) {
         if (i && (i & 63) == 0) {
             load_scales();
             __builtin_amdgcn_s_waitcnt(0x0F70);
@@ -457,8 +464,8 @@ __global__ __launch_bounds__(64 * kAttWaves, kv8_waves(D, NR)) void kv8_attentio
         }
         const float c = __int_as_float(__builtin_amdgcn_readlane(__float_as_int(k_scales), i & 63)) * a.scale;
         const float v_scale = __int_as_float(__builtin_amdgcn_readlane(__float_as_int(v_scales), i & 63));
-        if (base + kAttSpan < to) {
-            request(base + kAttSpan, buf ^ 1);
+        if (base + 32 * W < to) {
+            request(base + 32 * W, buf ^ 1);
             asm volatile("" ::: "memory");
             __builtin_amdgcn_s_waitcnt(0x0F70 | ((2 * kLoads) & 15) | ((2 * kLoads) >> 4 << 14));  // all but the requests just made
         } else {
@@ -571,7 +578,7 @@ __global__ __launch_bounds__(64 * kAttWaves, kv8_waves(D, NR)) void kv8_attentio
 
     // the wavefronts' results meet in LDS
     float* mo = reinterpret_cast<float*>(smem);                                  // [wave][kRows][kORow]
-    float2* mstat = reinterpret_cast<float2*>(mo + kAttWaves * kRows * kORow);  // [wave][kRows]
+    float2* mstat = reinterpret_cast<float2*>(mo + W * kRows * kORow);  // [wave][kRows]
     __syncthreads();
 #pragma unroll
     for (int t = 0; t < NR; ++t) {
@@ -584,14 +591,14 @@ __global__ __launch_bounds__(64 * kAttWaves, kv8_waves(D, NR)) void kv8_attentio
     }
     __syncthreads();
 #pragma unroll
-    for (int t = 0; t < NR; ++t) {
-        const int mine = 16 * t + (tid >> 4), row = first + mine;  // sixteen threads a row
-        if (row < n_used) {
-            float w[kAttWaves], top = -3.0e38f, all = 0.f;
+    for (int t = 0; t < kRows; t += 4 * W) {
+        const int mine = t + (tid >> 4), row = first + mine;  // sixteen threads a row
+        if (mine < kRows && row < n_used) {
+            float w[W], top = -3.0e38f, all = 0.f;
 #pragma unroll
-            for (int i = 0; i < kAttWaves; ++i) top = fmaxf(top, mstat[kRows * i + mine].x);
+            for (int i = 0; i < W; ++i) top = fmaxf(top, mstat[kRows * i + mine].x);
 #pragma unroll
-            for (int i = 0; i < kAttWaves; ++i) {
+            for (int i = 0; i < W; ++i) {
                 const float2 st = mstat[kRows * i + mine];
                 w[i] = __builtin_amdgcn_exp2f(st.x - top);
                 all += w[i] * st.y;
@@ -600,7 +607,7 @@ __global__ __launch_bounds__(64 * kAttWaves, kv8_waves(D, NR)) void kv8_attentio
             // a row that attends to nothing is zero
             const float inv = pos0 + token < 0 ? 0.f : 1.0f / all;
             const size_t slot = ((size_t)unit * a.c.n_kv + grp) * kRows + mine;
-            if ((tid & 15) == 0) {
+            if (W == kCutWaves && (tid & 15) == 0) {
                 if (cuts > 1) a.stat[slot] = make_float2(top, all);
                 uint4* join = a.join + ((size_t)u.seq * a.max_new + token) * (a.c.n_kv * rep) + grp * rep + (row - token * rep);
                 if (cut == 0) *reinterpret_cast<uint2*>(join) = make_uint2(unit, cuts_whole | (cuts > cuts_whole ? kRest : 0u));
@@ -611,7 +618,7 @@ __global__ __launch_bounds__(64 * kAttWaves, kv8_waves(D, NR)) void kv8_attentio
                 if (d >= D_used) break;
                 f32x4 x = f32x4{0.f, 0.f, 0.f, 0.f};
 #pragma unroll
-                for (int i = 0; i < kAttWaves; ++i) x += *reinterpret_cast<const f32x4*>(mo + (kRows * i + mine) * kORow + d) * w[i];
+                for (int i = 0; i < W; ++i) x += *reinterpret_cast<const f32x4*>(mo + (kRows * i + mine) * kORow + d) * w[i];
                 if (cuts > 1) {
                     *reinterpret_cast<f32x4*>(a.part + slot * D + d) = x;
                 } else {
@@ -721,7 +728,7 @@ Kv8Plan kv8_plan(int n_heads, int n_kv, int head_dim, int n_seq, int max_new) {
     p.dim = head_dim <= 64 ? 64 : head_dim <= 128 ? 128 : 256;
     p.nr = rows <= 16 || p.dim == 256 ? 1 : rows <= 32 || p.dim == 128 ? 2 : 4;
     const int kv = n_kv;
-    const int by_lds = 163840 / kv8_lds(p.dim, p.nr), by_registers = kv8_waves(p.dim, p.nr);
+    const int by_lds = 163840 / kv8_lds(p.dim, p.nr, kCutWaves), by_registers = kv8_waves(p.dim, p.nr, kCutWaves);
     p.places = (std::min(by_lds, by_registers) * device_cu_count() + kv - 1) / kv;
     p.tiles = (rows + 16 * p.nr - 1) / (16 * p.nr);
     // units: sum of tiles * ceil(spans / stretch) <= sum of tiles * spans / stretch + sum of tiles
@@ -748,24 +755,38 @@ hipError_t launch_kv8_attention(const Kv8Args& c, const uint16_t* q, int64_t q_s
     const uint64_t by_rows = (uint64_t)n_rows * rep / (16 * p.nr) + (uint64_t)(n_seq < n_rows ? n_seq : n_rows), by_seq = (uint64_t)n_seq * p.tiles;
     const uint64_t tiles = by_rows < by_seq ? by_rows : by_seq, spans = (uint64_t)((c.max_pos + kAttSpan - 1) / kAttSpan);
     const uint64_t most = 2 * tiles <= (uint64_t)p.places ? (uint64_t)p.places : 2 * (uint64_t)p.places + tiles;
-    const dim3 grid((unsigned)((tiles * spans < most ? tiles * spans : most) * c.n_kv));
+    // A cache of up to 1024 positions is four steps of eight wavefronts at most: less than the second launch, which joins what was cut, as long as
+    // the workgroups find a place at once or in turns (one token against 429 positions WHOLE1 / CUT1 us, 32 requests against 1000 WHOLE2 / CUT2).
+    const bool whole = p.dim <= 128 && c.max_pos <= 1024 && tiles * c.n_kv <= 2u * (unsigned)device_cu_count();
+    const dim3 grid((unsigned)((whole ? tiles : tiles * spans < most ? tiles * spans : most) * c.n_kv));
     // (row, query head) pairs; few of them have many stretches each: four wavefronts
     const uint64_t pairs = (uint64_t)n_seq * max_new * n_heads;
     const bool wide = pairs <= 8u * (unsigned)device_cu_count();
     const dim3 join((unsigned)(wide ? pairs : (pairs + 3) / 4));
-#define SD2_KV8(DIM, R)                                                                                                   \
-    if (p.dim == DIM && p.nr == R) {                                                                                      \
-        static std::atomic<uint64_t> done{0};                                                                             \
-        const hipError_t e = allow_lds(reinterpret_cast<const void*>(&kv8_attention_kernel<DIM, R>), kv8_lds(DIM, R), done); \
-        if (e != hipSuccess) return e;                                                                                    \
-        hipLaunchKernelGGL((kv8_attention_kernel<DIM, R>), grid, dim3(64 * kAttWaves), kv8_lds(DIM, R), s, a);               \
+#define SD2_KV8_ATTEND(DIM, R, W)                                                                                                \
+    do {                                                                                                                         \
+        static std::atomic<uint64_t> done{0};                                                                                    \
+        const hipError_t e = allow_lds(reinterpret_cast<const void*>(&kv8_attention_kernel<DIM, R, W>), kv8_lds(DIM, R, W), done); \
+        if (e != hipSuccess) return e;                                                                                           \
+        hipLaunchKernelGGL((kv8_attention_kernel<DIM, R, W>), grid, dim3(64 * W), kv8_lds(DIM, R, W), s, a);                     \
+    } while (0)
+#define SD2_KV8_CUT(DIM, R)                                                                                               \
+    do {                                                                                                                  \
+        SD2_KV8_ATTEND(DIM, R, kCutWaves);                                                                                \
         if (c.max_pos > kAttSpan && wide) hipLaunchKernelGGL((kv8_combine_kernel<DIM, R, 4>), join, dim3(256), 0, s, a);  \
         if (c.max_pos > kAttSpan && !wide) hipLaunchKernelGGL((kv8_combine_kernel<DIM, R, 1>), join, dim3(256), 0, s, a); \
+    } while (0)
+#define SD2_KV8(DIM, R)                                            \
+    if (p.dim == DIM && p.nr == R) {                               \
+        if (whole) SD2_KV8_ATTEND(DIM, R, kWholeWaves);            \
+        else SD2_KV8_CUT(DIM, R);                                  \
     }
     SD2_KV8(64, 1) SD2_KV8(64, 2) SD2_KV8(64, 4)
     SD2_KV8(128, 1) SD2_KV8(128, 2)
-    SD2_KV8(256, 1)
+    if (p.dim == 256) SD2_KV8_CUT(256, 1);
 #undef SD2_KV8
+#undef SD2_KV8_CUT
+#undef SD2_KV8_ATTEND
     return hipGetLastError();
 }
 

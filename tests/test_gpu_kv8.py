@@ -210,7 +210,7 @@ def check_attention(out, q, k, v, n_heads, lens, pos0, dim, max_new=64):
 @pytest.mark.parametrize("n_heads,n_kv,dim", HEADS)
 @pytest.mark.parametrize("lens,pos0,max_pos", [
     ([1], [0], 32), ([1], [30], 32), ([1, 1], [31, 32], 128), ([5], [428], 1024), ([8, 0, 3, 1], [127, 40, 128, 300], 352), ([64], [0], 64),
-    ([33, 64, 17], [0, 70, 255], 288), ([1, 5], [1500, 3], 1536), ([6, 4], [-3, -4], 32), ([6], [60], 64)])
+    ([33, 64, 17], [0, 70, 255], 288), ([8, 5], [1000, 1019], 1024), ([1, 5], [1500, 3], 1536), ([33, 17, 1, 0], [1290, 40, 0, 7], 1344), ([6, 4], [-3, -4], 32), ([6], [60], 64)])
 def test_attention(n_heads, n_kv, dim, lens, pos0, max_pos):
     history = [min(p, max_pos - n) for p, n in zip(pos0, lens)]  # the last case's rows reach past the cache
     slots, q, k, v = filled(lens, history, n_heads, n_kv, dim, max_pos)
@@ -284,10 +284,11 @@ def test_attention_of_the_first_rows_only():
 
 @pytest.mark.parametrize("dim", [64, 128, 256])
 @pytest.mark.parametrize("where", [41, 43])
-def test_nan_of_a_later_token_does_not_reach_earlier_rows(dim, where):
+@pytest.mark.parametrize("max_pos", [64, 1056])  # a cache that is not cut, and one that may be
+def test_nan_of_a_later_token_does_not_reach_earlier_rows(dim, where, max_pos):
     """A draft's value is NaN: rows that attend to it have NaN in that dimension, the others the result without it."""
     lens, pos0 = [5], [40]
-    slots, q, k, v = filled(lens, pos0, 4, 2, dim, 64)
+    slots, q, k, v = filled(lens, pos0, 4, 2, dim, max_pos)
     slots.v[0, 1, where, 3] = 0xFF
     slots.v[0, 0, where, dim - 1] = 0x7F
     v[0][1, where, 3] = v[0][0, where, dim - 1] = np.nan
@@ -296,9 +297,10 @@ def test_nan_of_a_later_token_does_not_reach_earlier_rows(dim, where):
     assert np.isnan(f64(out)).sum() == 4 * (45 - where)
 
 
-def test_nan_key_reaches_the_rows_that_attend_to_it():
+@pytest.mark.parametrize("max_pos", [64, 1056])
+def test_nan_key_reaches_the_rows_that_attend_to_it(max_pos):
     lens, pos0 = [4], [30]
-    slots, q, k, v = filled(lens, pos0, 2, 1, 64, 64)
+    slots, q, k, v = filled(lens, pos0, 2, 1, 64, max_pos)
     slots.k[0, 0, 32, 5] = 0x7F
     k[0][0, 32, 5] = np.nan
     out = attend(slots, q, 2, lens, pos0, n_rows=4)
@@ -354,9 +356,10 @@ def test_offsets_past_32_bits():
             assert (np.abs(out[i].reshape(8, dim)[g] - want) <= 3 * BF16_HALF * (w @ np.abs(vv)) + 1e-30).all()
 
 
-def test_captured_call_serves_new_lengths():
+@pytest.mark.parametrize("max_pos", [512, 2048])
+def test_captured_call_serves_new_lengths(max_pos):
     """A graph of append and attention; between replays the offsets, positions and rows change, and so do the results."""
-    n_heads, n_kv, dim, max_pos = 6, 2, 128, 512
+    n_heads, n_kv, dim = 6, 2, 128
     slots = Slots(3, n_kv, max_pos, dim)
     width = (n_heads + 2 * n_kv) * dim
     x = torch.zeros((8, width), device="cuda")
@@ -396,11 +399,12 @@ def test_captured_call_serves_new_lengths():
         whole = [w + n for w, n in zip(whole, lens)]
 
 
-def test_two_streams_at_once():
+@pytest.mark.parametrize("max_pos", [1024, 1056])
+def test_two_streams_at_once(max_pos):
     """Two calls that may overlap, each with its own workspace, give what they give one after the other."""
     lens, pos0 = [5, 3], [900, 30]
-    a, qa, _, _ = filled(lens, pos0, 8, 2, 128, 1024, seed=61)
-    b, qb, _, _ = filled(lens, pos0, 8, 2, 128, 1024, seed=62)
+    a, qa, _, _ = filled(lens, pos0, 8, 2, 128, max_pos, seed=61)
+    b, qb, _, _ = filled(lens, pos0, 8, 2, 128, max_pos, seed=62)
     want = [attend(s, q, 8, lens, pos0, n_rows=8) for s, q in ((a, qa), (b, qb))]
     nb = sd2.kv8_attention_workspace_size(a.c, 8, 2, 5)
     ws, out = [torch.empty(nb, dtype=torch.uint8, device="cuda") for _ in range(2)], [torch.full_like(want[0], 7.0) for _ in range(2)]

@@ -220,8 +220,8 @@ hipError_t launch_kv8_append(const Kv8Args& c, const float* qkv, int n_heads, co
 // leave it by the transposing read.  Weights are rounded to bf16 for the second product, at most 2^-8 of a weight.
 //
 // Bound by bytes where there are many positions: 59 requests with 226 000 positions in 16 heads of keys and values of 128 (464 MB) 95 us,
-// 4.9 TB/s, where a pure read has 5.35 (and 5 us to join); by the chain plan - first tile - scores - meeting - join where there are few: one token against 429
-// positions 8.3 us, five against 30016 15 us.  64 tokens with four query heads a group: 1.9 us for 128 positions of 64 rows, softmax and
+// 4.9 TB/s, where a pure read has 5.35 (and 5 us to join); by the chain plan - first tile - scores - meeting (- join) where there are few: one token against
+// 429 positions 6.8 us, five against 30016 15 us.  64 tokens with four query heads a group: 1.9 us for 128 positions of 64 rows, softmax and
 // conversions on the vector ALU.
 constexpr int kCutWaves = 4, kWholeWaves = 8;  // wavefronts of a workgroup that takes a stretch, and of one that takes all positions
 constexpr int kAttSpan = 32 * kCutWaves;        // positions of four tiles side by side: what stretches are made of
@@ -755,13 +755,16 @@ hipError_t launch_kv8_attention(const Kv8Args& c, const uint16_t* q, int64_t q_s
     const uint64_t by_rows = (uint64_t)n_rows * rep / (16 * p.nr) + (uint64_t)(n_seq < n_rows ? n_seq : n_rows), by_seq = (uint64_t)n_seq * p.tiles;
     const uint64_t tiles = by_rows < by_seq ? by_rows : by_seq, spans = (uint64_t)((c.max_pos + kAttSpan - 1) / kAttSpan);
     const uint64_t most = 2 * tiles <= (uint64_t)p.places ? (uint64_t)p.places : 2 * (uint64_t)p.places + tiles;
-    // A cache of up to 1024 positions is four steps of eight wavefronts at most: less than the second launch, which joins what was cut, as long as
-    // the workgroups find a place at once or in turns (one token against 429 positions WHOLE1 / CUT1 us, 32 requests against 1000 WHOLE2 / CUT2).
-    const bool whole = p.dim <= 128 && c.max_pos <= 1024 && tiles * c.n_kv <= 2u * (unsigned)device_cu_count();
+    // A cache of up to 1024 positions is four steps of eight wavefronts at most, less than the second launch that joins what was cut; up to 2048
+    // it is where the workgroups fill a quarter of the chip.  (Whole / cut, us: 24 query heads over 8, one token against 429 positions
+    // 6.8 / 8.3, against 1000 9.0 / 8.4, against 1900 12.5 / 8.5; 32 drafts of five against 500 10.1 / 15.4, against 1800 25 / 31; 64 against 0 to
+    // 1900 23 / 30; eight chunks of 64 against 1800 35 / 45.  Far more workgroups than places: 32 chunks against 500 59 / 51.)
+    const uint64_t wholes = tiles * (uint64_t)c.n_kv, cus = (uint64_t)device_cu_count();
+    const bool whole = p.dim <= 128 && wholes <= 4 * cus && (c.max_pos <= 1024 || (c.max_pos <= 2048 && 4 * wholes >= cus));
     const dim3 grid((unsigned)((whole ? tiles : tiles * spans < most ? tiles * spans : most) * c.n_kv));
     // (row, query head) pairs; few of them have many stretches each: four wavefronts
     const uint64_t pairs = (uint64_t)n_seq * max_new * n_heads;
-    const bool wide = pairs <= 8u * (unsigned)device_cu_count();
+    const bool wide = pairs <= 8 * cus;
     const dim3 join((unsigned)(wide ? pairs : (pairs + 3) / 4));
 #define SD2_KV8_ATTEND(DIM, R, W)                                                                                                \
     do {                                                                                                                         \

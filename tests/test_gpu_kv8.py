@@ -217,6 +217,16 @@ def test_attention(n_heads, n_kv, dim, lens, pos0, max_pos):
     check_attention(attend(slots, q, n_heads, lens, pos0, n_rows=sum(lens)), q, k, v, n_heads, lens, pos0, dim)
 
 
+@pytest.mark.parametrize("n_heads,n_kv,dim", [(24, 8, 128), (32, 8, 64), (24, 8, 112)])
+@pytest.mark.parametrize("max_new", [1, 5, 64])
+def test_attention_of_caches_between_one_and_two_thousand_positions(n_heads, n_kv, dim, max_new):
+    """So many workgroups that these are not cut either."""
+    pos0 = [1200, 0, 700, 33, 1400, 255, 256, 90, 1024, 5, 800, 1300]
+    lens = [max(max_new - i % 3, 1) for i in range(12)]
+    slots, q, k, v = filled(lens, pos0, n_heads, n_kv, dim, 1472)
+    check_attention(attend(slots, q, n_heads, lens, pos0, n_rows=sum(lens)), q, k, v, n_heads, lens, pos0, dim)
+
+
 @pytest.mark.parametrize("n_heads,n_kv", [(1, 1), (64, 1), (20, 20)])
 def test_attention_few_and_many_heads_a_group(n_heads, n_kv):
     lens, pos0 = [2, 9], [200, 77]

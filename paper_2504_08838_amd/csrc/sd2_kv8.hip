@@ -214,15 +214,16 @@ hipError_t launch_kv8_append(const Kv8Args& c, const float* qkv, int n_heads, co
 //
 // The rows of a workgroup are (token, query head of the group) pairs in that order, up to 16 NR of them, so that a cached position
 // is read and converted once for all of them.  A workgroup takes a stretch of positions, its four wavefronts every fourth tile of
-// 32 -- one block, so a tile has one scale; short caches are not cut, and eight wavefronts take all of one.  Scores come out transposed (positions by rows): a lane then holds eight positions of one
-// row, which is how the next product wants its operand, so weights never leave the registers.  Positions are dealt to the rows of the
-// first product such that those eight follow one another.  Tiles go from memory straight into LDS, one ahead of the one at work, and values
-// leave it by the transposing read.  Weights are rounded to bf16 for the second product, at most 2^-8 of a weight.
+// 32 -- one block, so a tile has one scale; short caches are not cut, and eight wavefronts take all of one.  Scores come out transposed
+// (positions by rows): a lane then holds eight positions of one row, which is how the next product wants its operand, so weights never
+// leave the registers.  Positions are dealt to the rows of the first product such that those eight follow one another.  Tiles go from
+// memory straight into LDS, one ahead of the one at work, and values leave it by the transposing read.  Weights are rounded to bf16 for
+// the second product, at most 2^-8 of a weight.
 //
 // Bound by bytes where there are many positions: 59 requests with 226 000 positions in 16 heads of keys and values of 128 (464 MB) 95 us,
-// 4.9 TB/s, where a pure read has 5.35 (and 5 us to join); by the chain plan - first tile - scores - meeting (- join) where there are few: one token against
-// 429 positions 6.8 us, five against 30016 15 us.  64 tokens with four query heads a group: 1.9 us for 128 positions of 64 rows, softmax and
-// conversions on the vector ALU.
+// 4.9 TB/s, where a pure read has 5.35 (and 5 us to join); by the chain plan - first tile - scores - meeting (- join) where there are few:
+// one token against 429 positions 6.8 us, five against 30016 15 us.  64 tokens with four query heads a group: 1.9 us for 128 positions of
+// 64 rows, softmax and conversions on the vector ALU.
 constexpr int kCutWaves = 4, kWholeWaves = 8;  // wavefronts of a workgroup that takes a stretch, and of one that takes all positions
 constexpr int kAttSpan = 32 * kCutWaves;        // positions of four tiles side by side: what stretches are made of
 

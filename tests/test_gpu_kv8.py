@@ -444,6 +444,20 @@ def test_offsets_that_break_the_rules_stay_inside_the_buffers():
     assert (rows[8:] == 7.0).all() and (whole[8:] == 7.0).all() and (slots.k[3] == 0x7F).all() and (slots.v[3] == 0x7F).all()
 
 
+def test_offsets_that_break_the_rules_where_stretches_are_joined():
+    """Sequences that share rows, more of them than the rows allow, and a workspace whose records nobody wrote: nothing outside."""
+    slots = Slots(6, 1, 4096, 64)
+    whole = torch.full((36, 4 * 64), 7.0, dtype=torch.bfloat16, device="cuda")
+    rows = torch.ones((36, 6 * 64), dtype=torch.bfloat16, device="cuda")
+    rs, p0 = i32([0, 32, 0, 32, 0, 32, 0]), i32([4000, -(1 << 31), 3000, (1 << 31) - 1, 4095, 0])
+    nb = sd2.kv8_attention_workspace_size(slots.c, 4, 6, 32)
+    for fill in (0xFF, 0x00, 0x01):
+        ws = torch.full((nb + 4096,), fill, dtype=torch.uint8, device="cuda")
+        sd2.kv8_attention(slots.c, rows.data_ptr(), 6 * 64, 4, rs.data_ptr(), p0.data_ptr(), 6, 32, 32, whole.data_ptr(), ws.data_ptr(), nb, gu.stream_ptr())
+        torch.cuda.synchronize()
+        assert (whole[32:] == 7.0).all() and (ws[nb:] == fill).all()
+
+
 def test_the_path_of_a_layer():
     """q|k|v linear, append, prompt attention, output linear; then drafts against the cache: as a serving program runs them, against the
     oracle link by link (every link takes the library's own values of the link before)."""

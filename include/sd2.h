@@ -298,8 +298,8 @@ int sd2_sparse_drafter_decode(const sd2_model_t* model, const uint16_t* h_in_bf1
  * A value is its code times its block's scale.  The scale of a block is the smallest 2^e, e >= -100, for which the largest finite
  * magnitude among its positions is at most 448 * 2^e; codes are rounded to nearest, ties to even.  When further positions enter a
  * block and need a larger scale, the codes that are there are rounded to it (none ever returns to a smaller one).  Infinities
- * and NaN become NaN (either code) and do not count for the scale; a value beyond 2^127 may round up to an infinity.  A cache needs
- * no initial contents.
+ * and NaN become NaN (either code) and do not count for the scale; a value of nearly 2^128 rounds up to 2^128 (256 * 2^120), which
+ * attention takes as that number.  A cache needs no initial contents.
  * head_dim: a multiple of 16, at most 256.  max_pos: a multiple of SD2_KV8_BLOCK, at most 2^20.  n_slots, n_kv, n_heads:
  * at most 65536, 4096, 4096, and at most 64 query heads for each key/value head.  All pointers 16-byte aligned. */
 #define SD2_KV8_BLOCK 32

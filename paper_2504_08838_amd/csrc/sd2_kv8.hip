@@ -229,6 +229,11 @@ constexpr int kAttSpan = 32 * kCutWaves;        // positions of four tiles side 
 
 constexpr uint32_t kRest = 0x80000000u;
 
+// Values enter the second product at 2^-8 of their size, and results are multiplied by 2^8 at the end.  The largest that is
+// stored is 256 * 2^120, more than bf16 and fp32 have: as an infinity, it would be NaN in the rows whose weight for it is zero.  The smallest, 2^-109,
+// stays a normal number.
+constexpr float kValuesIn = 0x1p-8f, kResultsOut = 0x1p8f;
+
 struct Kv8AttArgs {
     Kv8Args c;
     const uint16_t* q;
@@ -464,7 +469,7 @@ __global__ __launch_bounds__(64 * W, kv8_waves(D, NR, W)) void kv8_attention_ker
             asm volatile("" : "+v"(k_scales), "+v"(v_scales)::"memory");
         }
         const float c = __int_as_float(__builtin_amdgcn_readlane(__float_as_int(k_scales), i & 63)) * a.scale;
-        const float v_scale = __int_as_float(__builtin_amdgcn_readlane(__float_as_int(v_scales), i & 63));
+        const float v_scale = __int_as_float(__builtin_amdgcn_readlane(__float_as_int(v_scales), i & 63)) * kValuesIn;
         if (base + 32 * W < to) {
             request(base + 32 * W, buf ^ 1);
             asm volatile("" ::: "memory");
@@ -606,7 +611,7 @@ __global__ __launch_bounds__(64 * W, kv8_waves(D, NR, W)) void kv8_attention_ker
             }
             const int token = row / rep;
             // a row that attends to nothing is zero
-            const float inv = pos0 + token < 0 ? 0.f : 1.0f / all;
+            const float inv = pos0 + token < 0 ? 0.f : kResultsOut / all;
             const size_t slot = ((size_t)unit * a.c.n_kv + grp) * kRows + mine;
             if (W == kCutWaves && (tid & 15) == 0) {
                 if (cuts > 1) a.stat[slot] = make_float2(top, all);
@@ -717,7 +722,7 @@ __global__ __launch_bounds__(256) void kv8_combine_kernel(Kv8AttArgs a) {
     }
     if (!used) return;
     // a row that attends to nothing is zero
-    x *= (int64_t)sr.pos0 + token < 0 ? 0.f : 1.0f / all;
+    x *= (int64_t)sr.pos0 + token < 0 ? 0.f : kResultsOut / all;
     *reinterpret_cast<uint2*>(a.out + ((size_t)(sr.start + token) * n_heads + h) * a.c.head_dim + d) =
         make_uint2(pack_bf16(x[0], x[1]), pack_bf16(x[2], x[3]));
 }

@@ -318,6 +318,26 @@ def test_nan_key_reaches_the_rows_that_attend_to_it(max_pos):
     assert torch.isnan(out[2:4].float()).all() and torch.isfinite(out[:2].float()).all()
 
 
+@pytest.mark.parametrize("dim", [64, 128, 256])
+@pytest.mark.parametrize("max_pos,pos0", [(64, 40), (1056, 40), (4096, 700)])  # not cut, in one stretch, in stretches that are joined
+def test_values_stored_as_a_number_that_bf16_does_not_have(dim, max_pos, pos0):
+    """Drafts' values of nearly 2^128 are stored as 256 times 2^120, more than bf16 and fp32 hold.  Rows in front of them have the result
+    without them, the others their part of them, which is finite."""
+    n_heads, n_kv, lens = 4, 2, [5]
+    slots, q, _, _ = filled([1], [pos0 - 1], n_heads, n_kv, dim, max_pos)
+    q = torch.cat([q, q * 0.5])[:5]
+    x = qkv(71, 5, n_heads, n_kv, dim)
+    at = (n_heads + n_kv) * dim
+    x[1, at + dim + 3], x[3, at + dim - 1] = 3.38e38, -3.38e38
+    before = slots.host()
+    rows = append(slots, x, n_heads, lens, [pos0])
+    check_store(before, slots, rows, n_heads, lens, [pos0])
+    k, v, ks, vs = slots.host()
+    assert v[0, 1, pos0 + 1, 3] == 0x78 and v[0, 0, pos0 + 3, dim - 1] == 0xF8 and (vs[0, :, (pos0 + 1) // 32] == 2.0 ** 120).all()
+    k, v = [kv8.values(k[0], ks[0])], [kv8.values(v[0], vs[0])]
+    check_attention(attend(slots, q, n_heads, lens, [pos0]), q, k, v, n_heads, lens, [pos0], dim)
+
+
 def test_large_scores():
     """Scores of thousands: one position takes all the weight, and every running maximum is left far behind."""
     lens, pos0 = [3], [500]

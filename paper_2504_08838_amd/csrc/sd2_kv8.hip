@@ -645,7 +645,7 @@ __global__ __launch_bounds__(256) void kv8_combine_kernel(Kv8AttArgs a) {
     __shared__ __attribute__((aligned(16))) float sums[W > 1 ? kSide : 1][W > 1 ? D : 1];
     __shared__ float2 stats[W > 1 ? kSide : 1];
     const int n_heads = a.c.n_kv * a.rep, tid = threadIdx.x & (64 * W - 1);
-    const uint32_t item = blockIdx.x * (4 / W) + (W > 1 ? 0u : (uint32_t)__builtin_amdgcn_readfirstlane((int)threadIdx.x >> 6));
+    const uint32_t item = folded_block() * (4 / W) + (W > 1 ? 0u : (uint32_t)__builtin_amdgcn_readfirstlane((int)threadIdx.x >> 6));
     const uint32_t h = item % (uint32_t)n_heads, row = item / (uint32_t)n_heads;  // row: sequence times max_new + token
     if (row >= (uint32_t)a.n_seq * (uint32_t)a.max_new) return;
     const uint4 join = a.join[(size_t)row * n_heads + h];
@@ -771,7 +771,7 @@ hipError_t launch_kv8_attention(const Kv8Args& c, const uint16_t* q, int64_t q_s
     // (row, query head) pairs; few of them have many stretches each: four wavefronts
     const uint64_t pairs = (uint64_t)n_seq * max_new * n_heads;
     const bool wide = pairs <= 8 * cus;
-    const dim3 join((unsigned)(wide ? pairs : (pairs + 3) / 4));
+    const dim3 join = folded_grid(wide ? pairs : (pairs + 3) / 4);
 #define SD2_KV8_ATTEND(DIM, R, W)                                                                                                \
     do {                                                                                                                         \
         static std::atomic<uint64_t> done{0};                                                                                    \

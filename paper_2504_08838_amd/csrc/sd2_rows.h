@@ -23,6 +23,15 @@ inline hipError_t allow_lds(const void* kernel, int bytes, std::atomic<uint64_t>
     return e;
 }
 
+// Grids of any number of workgroups: HIP launches fewer than 2^32 threads in a dimension, so those past 2^22 go into a second one.  The
+// last row of a folded grid may be longer than what is left: kernels end workgroups without work by themselves.
+constexpr int kGridFold = 22;
+inline dim3 folded_grid(uint64_t workgroups) {
+    const uint64_t row = (uint64_t)1 << kGridFold;
+    return workgroups <= row ? dim3((unsigned)workgroups) : dim3((unsigned)row, (unsigned)((workgroups + row - 1) >> kGridFold));
+}
+__device__ __forceinline__ uint32_t folded_block() { return blockIdx.y << kGridFold | blockIdx.x; }
+
 struct SeqRows {
     int start, count, pos0;  // first row, rows, position of the first row
 };

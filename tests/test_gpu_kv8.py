@@ -524,3 +524,31 @@ def test_the_path_of_a_layer():
         ref = f64(out) @ dense[1].T
         assert np.linalg.norm(o.cpu().numpy() - ref) <= 1e-3 * np.linalg.norm(ref)
         done = [d + m for d, m in zip(done, new)]
+
+
+def test_more_rows_to_join_than_a_grid_dimension_has_threads():
+    """16384 sequences of up to 64 rows of 64 heads: 2^26 of them may have been cut, four a workgroup of 256 threads.  Three sequences have
+    rows, the first, the last and one in between."""
+    n_seq, n_heads, dim, max_pos, n_rows = 16384, 64, 16, 160, 1024
+    some = {0: (64, 90), 9000: (5, 150), n_seq - 1: (59, 96)}  # rows, position of the first
+    slots = Slots(n_seq, 1, max_pos, dim)
+    gen = torch.Generator(device="cuda")
+    gen.manual_seed(81)
+    lens, pos0 = np.zeros(n_seq, dtype=np.int64), np.zeros(n_seq, dtype=np.int64)
+    for b, (n, p) in some.items():
+        lens[b], pos0[b] = n, p
+        for c in (slots.k, slots.v):
+            c[b] = (torch.randn(c[b].shape, generator=gen, device="cuda") * 95).clamp_(-448, 448).to(torch.float8_e4m3fn).view(torch.uint8)
+        slots.ks[b], slots.vs[b] = 2.0 ** -7, 2.0 ** -8
+    q = torch.randn(n_rows, n_heads * dim, generator=gen, device="cuda").to(torch.bfloat16)
+    rs, p0 = i32(np.concatenate([[0], np.cumsum(lens)]).tolist()), i32(pos0.tolist())
+    out = torch.full((n_rows, n_heads * dim), 7.0, dtype=torch.bfloat16, device="cuda")
+    nb = sd2.kv8_attention_workspace_size(slots.c, n_heads, n_seq, 64)
+    ws = torch.empty(nb, dtype=torch.uint8, device="cuda")  # 17 GiB
+    sd2.kv8_attention(slots.c, q.data_ptr(), q.stride(0), n_heads, rs.data_ptr(), p0.data_ptr(), n_seq, n_rows, 64, out.data_ptr(), ws.data_ptr(), nb,
+                      gu.stream_ptr())
+    torch.cuda.synchronize()
+    del ws
+    torch.cuda.empty_cache()
+    k, v = ([kv8.values(c[b].cpu().numpy(), s[b].cpu().numpy()) for b in some] for c, s in ((slots.k, slots.ks), (slots.v, slots.vs)))
+    check_attention(out, q, k, v, n_heads, [n for n, _ in some.values()], [p for _, p in some.values()], dim)

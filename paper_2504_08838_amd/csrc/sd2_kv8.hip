@@ -349,8 +349,9 @@ __global__ __launch_bounds__(64 * W, kv8_waves(D, NR, W)) void kv8_attention_ker
     constexpr int kORow = D + 4;  // floats
     extern __shared__ __attribute__((aligned(16))) uint8_t smem[];  // [wave][buffer][keys, values][32][D]
     const int tid = threadIdx.x, lane = tid & 63, wave = __builtin_amdgcn_readfirstlane(tid >> 6), n = lane & 15, g = lane >> 4;
-    const int grp = blockIdx.x % a.c.n_kv;
-    const uint32_t unit = blockIdx.x / a.c.n_kv;
+    const uint32_t block = folded_block(), n_kv = (uint32_t)a.c.n_kv, unit = block / n_kv;
+    const int grp = (int)(block - unit * n_kv);
+    if (unit >= a.bound) return;  // offsets that break the rules can have more units than the workspace has room for
     const Sequences seqs(a.row_start, a.pos0, a.n_seq, a.n_rows);
     bool many = false;
     uint32_t stretch = 1u << 13, n_whole = ~0u;  // as many spans as the longest cache has
@@ -767,7 +768,7 @@ hipError_t launch_kv8_attention(const Kv8Args& c, const uint16_t* q, int64_t q_s
     // 1900 23 / 30; eight chunks of 64 against 1800 35 / 45.  Far more workgroups than places: 32 chunks against 500 59 / 51.)
     const uint64_t wholes = tiles * (uint64_t)c.n_kv, cus = (uint64_t)device_cu_count();
     const bool whole = p.dim <= 128 && wholes <= 4 * cus && (c.max_pos <= 1024 || (c.max_pos <= 2048 && 4 * wholes >= cus));
-    const dim3 grid((unsigned)((whole ? tiles : tiles * spans < most ? tiles * spans : most) * c.n_kv));
+    const dim3 grid = folded_grid((whole ? tiles : tiles * spans < most ? tiles * spans : most) * c.n_kv);
     // (row, query head) pairs; few of them have many stretches each: four wavefronts
     const uint64_t pairs = (uint64_t)n_seq * max_new * n_heads;
     const bool wide = pairs <= 8 * cus;

@@ -552,3 +552,30 @@ def test_more_rows_to_join_than_a_grid_dimension_has_threads():
     torch.cuda.empty_cache()
     k, v = ([kv8.values(c[b].cpu().numpy(), s[b].cpu().numpy()) for b in some] for c, s in ((slots.k, slots.ks), (slots.v, slots.vs)))
     check_attention(out, q, k, v, n_heads, [n for n, _ in some.values()], [p for _, p in some.values()], dim)
+
+
+def test_more_workgroups_than_a_grid_dimension_has_threads():
+    """4096 sequences of a token with 4096 key/value heads: 2^24 workgroups of 256 threads.  Every token attends to itself alone, so that its
+    result is its value."""
+    n_seq, n_heads, dim = 4096, 4096, 16
+    gen = torch.Generator(device="cuda")
+    gen.manual_seed(82)
+    slots = Slots(n_seq, n_heads, 32, dim)  # 16 GiB
+    for c in (slots.k, slots.v):
+        c[:, :, 0] = torch.randint(-60, 60, (n_seq, n_heads, dim), generator=gen, device="cuda").to(torch.float8_e4m3fn).view(torch.uint8)
+    slots.ks.fill_(2.0 ** -6)
+    slots.vs.copy_(torch.exp2(torch.randint(-9, 9, slots.vs.shape, generator=gen, device="cuda").float()))
+    q = torch.empty(n_seq, n_heads * dim, dtype=torch.bfloat16, device="cuda").normal_(generator=gen)
+    rs, p0 = i32(list(range(n_seq + 1))), i32([0] * n_seq)
+    out = torch.full_like(q, 7.0)
+    nb = sd2.kv8_attention_workspace_size(slots.c, n_heads, n_seq, 1)
+    ws = torch.empty(nb, dtype=torch.uint8, device="cuda")  # 66 GiB
+    sd2.kv8_attention(slots.c, q.data_ptr(), q.stride(0), n_heads, rs.data_ptr(), p0.data_ptr(), n_seq, n_seq, 1, out.data_ptr(), ws.data_ptr(), nb,
+                      gu.stream_ptr())
+    torch.cuda.synchronize()
+    del ws
+    want = (slots.v[:, :, 0].view(torch.float8_e4m3fn).float() * slots.vs).to(torch.bfloat16).view(n_seq, -1)
+    same = bool((out == want).all())
+    del slots, want, q, out
+    torch.cuda.empty_cache()
+    assert same

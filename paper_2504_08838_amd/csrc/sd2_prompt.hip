@@ -85,9 +85,10 @@ __global__ __launch_bounds__(64 * G * T, D < 256 ? 2 : 1) void prompt_attention_
     constexpr int kAhead = kTile * T;            // positions from a team's tile to its next
     extern __shared__ __attribute__((aligned(16))) uint8_t whole[];  // [team][kBuffers][keys, values][kBytes]
     const int tid = threadIdx.x, lane = tid & 63, wave = __builtin_amdgcn_readfirstlane(tid >> 6), n = lane & 31, h = lane >> 5;
-    const int grp = blockIdx.x % a.n_kv, rep = a.rep, hd = a.head_dim;
+    const uint32_t block = folded_block(), n_kv = (uint32_t)a.n_kv, unit = block / n_kv;
+    const int grp = (int)(block - unit * n_kv), rep = a.rep, hd = a.head_dim;
     auto tiles_of = [&](const SeqRows& r) { return (uint32_t)(r.count * rep + kRows - 1) / kRows; };
-    const SeqUnit u = Sequences(a.row_start, nullptr, a.n_seq, a.n_rows).find_largest_first(blockIdx.x / a.n_kv, tiles_of);
+    const SeqUnit u = Sequences(a.row_start, nullptr, a.n_seq, a.n_rows).find_largest_first(unit, tiles_of);
     if (u.seq < 0) return;
     const SeqRows sr = u.rows;
     const int n_used = sr.count * rep;
@@ -371,13 +372,13 @@ hipError_t launch_prompt_attention(const uint16_t* q, const uint16_t* k, const u
     const PromptArgs a = {q, k, v, q_stride, kv_stride, row_start, n_seq, n_rows, n_kv, rep, head_dim,
                           (float)(1.4426950408889634 / sqrt((double)head_dim)), out};
     const int64_t seqs = n_seq < n_rows ? n_seq : n_rows, cus = device_cu_count();
-    auto units = [&](int g) { return ((int64_t)n_rows * rep / (32 * g) + seqs) * n_kv; };
+    auto units = [&](int g) { return ((int64_t)n_rows * rep / (32 * g) + seqs) * n_kv; };  // each of up to 512 threads
 #define SD2_PROMPT(DIM, G, T)                                                                                                        \
     do {                                                                                                                             \
         static std::atomic<uint64_t> done{0};                                                                                        \
         const hipError_t e = allow_lds(reinterpret_cast<const void*>(&prompt_attention_kernel<DIM, G, T>), prompt_lds(DIM, G, T), done); \
         if (e != hipSuccess) return e;                                                                                               \
-        hipLaunchKernelGGL((prompt_attention_kernel<DIM, G, T>), dim3((unsigned)units(G)), dim3(64 * G * T), prompt_lds(DIM, G, T), s, a); \
+        hipLaunchKernelGGL((prompt_attention_kernel<DIM, G, T>), folded_grid(units(G)), dim3(64 * G * T), prompt_lds(DIM, G, T), s, a); \
     } while (0)
     // Which kernel, by what the host knows (us, 24 query heads over 8 of 128 dimensions unless said otherwise; 32 rows a workgroup and four
     // teams / 128 rows and two teams / 128 rows and one team):

@@ -249,3 +249,21 @@ def test_same_bits_every_time(n, repeats):
     for _ in range(repeats):
         run(*other, [n], 24, 8, 128)
         assert torch.equal(run(q, k, v, [n], 24, 8, 128).view(torch.int16), first)
+
+
+@pytest.mark.parametrize("n_heads,n_kv", [(4096, 4096), (4096, 2048)])
+def test_more_workgroups_than_a_grid_dimension_has_threads(n_heads, n_kv):
+    """Sequences of a token: 4096 with 4096 key/value heads, 8192 with 2048, 2^24 workgroups of 256 threads.  Every token attends to itself
+    alone, so that its result is its value."""
+    n_seq, dim = (1 << 24) // n_kv, 16
+    gen = torch.Generator(device="cuda")
+    gen.manual_seed(70)
+    q, k, v = (torch.empty(n_seq, h * dim, dtype=torch.bfloat16, device="cuda").normal_(generator=gen) for h in (n_heads, n_kv, n_kv))
+    rs, out = i32(list(range(n_seq + 1))), torch.full_like(q, 7.0)
+    sd2.prompt_attention(q.data_ptr(), k.data_ptr(), v.data_ptr(), q.stride(0), k.stride(0), rs.data_ptr(), n_seq, n_seq, n_heads, n_kv, dim,
+                         out.data_ptr(), gu.stream_ptr())
+    torch.cuda.synchronize()
+    same = bool((out.view(n_seq, n_kv, n_heads // n_kv, dim) == v.view(n_seq, n_kv, 1, dim)).all())
+    del q, k, v, out
+    torch.cuda.empty_cache()
+    assert same

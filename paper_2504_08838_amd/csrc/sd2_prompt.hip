@@ -97,8 +97,11 @@ __global__ __launch_bounds__(64 * G * T, D < 256 ? 2 : 1) void prompt_attention_
     uint8_t* smem = whole + team * kBuffers * 2 * kBytes;
     const int first = kRows * (int)u.index, wave_first = first + 32 * member;
     const int n_pos = min(first + kRows - 1, n_used - 1) / rep + 1;               // positions that the workgroup's rows attend to
-    // of the wavefront's own rows: positions that the last attends to, and the last position that all attend to (no rows: none)
-    const int wave_pos = wave_first < n_used ? min(wave_first + 31, n_used - 1) / rep + 1 : 0, wave_low = wave_first < n_used ? wave_first / rep : -1;
+    // positions that the last of the wavefront's own rows attends to (no rows: none)
+    const int wave_pos = wave_first < n_used ? min(wave_first + 31, n_used - 1) / rep + 1 : 0;
+    // Last position of the team's tiles in the steps that no mask touches, steps in which all rows attend to all positions.  Where steps have
+    // barriers, these are steps of all teams: the workgroup's wavefronts go from the one loop into the other together.
+    const int low = first / rep - (G == 1 ? 0 : kTile * (T - 1 - team));
     const uint16_t* kg = a.k + (size_t)sr.start * a.kv_stride + (size_t)grp * hd;
     const uint16_t* vg = a.v + (size_t)sr.start * a.kv_stride + (size_t)grp * hd;
 
@@ -282,9 +285,9 @@ __global__ __launch_bounds__(64 * G * T, D < 256 ? 2 : 1) void prompt_attention_
     // the queries with the first tile: a wait of the compiler's for them would be one for what is asked for behind them as well
     if (G == 1) wait_memory<0>();
     const int last = n_pos + kTile * team;           // as many steps for every team
-    for (; base < last && base + kTile - 1 <= wave_low; base += kAhead, buf ^= kBuffers - 1) {  // all rows attend to all positions
+    for (; base < last && base + kTile - 1 <= low; base += kAhead, buf ^= kBuffers - 1) {
         next();
-        tile(base, std::false_type());
+        if (G == 1 || wave_pos > 0) tile(base, std::false_type());
     }
     for (; base < last; base += kAhead, buf ^= kBuffers - 1) {
         next();

@@ -61,9 +61,13 @@ __device__ __forceinline__ int val_place(int r, int c) {
 
 // 16 bytes from base + offset of every lane to lds + 16 * lane.  As assembly, because the compiler waits for all such requests in front of
 // every transposing read of LDS: it cannot tell the buffers apart.  Nothing returns to registers; whoever reads the bytes waits first.
+// (m0 is never allocated, of which the compiler warns; named, it is known to be written.)
+#pragma clang diagnostic push
+#pragma clang diagnostic ignored "-Winline-asm"
 __device__ __forceinline__ void load_to_lds(const void* base, uint32_t offset, uint32_t lds) {
-    asm volatile("s_mov_b32 m0, %2\n\ts_nop 0\n\tglobal_load_lds_dwordx4 %0, %1" ::"v"(offset), "s"(base), "s"(lds) : "memory");
+    asm volatile("s_mov_b32 m0, %2\n\ts_nop 0\n\tglobal_load_lds_dwordx4 %0, %1" ::"v"(offset), "s"(base), "s"(lds) : "memory", "m0");
 }
+#pragma clang diagnostic pop
 
 // Waits for all but the last N vector memory operations, and for all operations on LDS; nothing moves across them.
 template <int N>

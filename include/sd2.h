@@ -289,7 +289,7 @@ int sd2_sparse_drafter_decode(const sd2_model_t* model, const uint16_t* h_in_bf1
  * Rows behind the last sequence's are neither read nor written.  pos0_dev (device int32 [n_seq]): the position of a
  * sequence's first row.  Both are read by the kernels, not by the host: a captured call serves whatever they hold when it is
  * replayed.  Values outside these rules give unspecified results, but no access outside the buffers.
- * n_seq and n_rows (0 .. 2^24) say how large the arrays are; n_rows * n_heads <= 2^30.  With no rows a call does nothing.
+ * n_seq (0 .. 65536) and n_rows (0 .. 2^24) say how large the arrays are; n_rows * n_heads <= 2^30.  With no rows a call does nothing.
  * Outputs must not overlap inputs.
  *
  * The cache of one layer: slot b belongs to sequence b.

@@ -1,5 +1,6 @@
 """Refusals of the packed-row operators and the 8-bit cache: on the host, before any launch (no GPU is needed)."""
 import ctypes as C
+import os
 
 import pytest
 
@@ -95,3 +96,18 @@ def test_no_rows_or_sequences_is_a_call_that_does_nothing():
         sd2.kv8_append(_cache(), *{**APPEND, **over}.values())
         sd2.prompt_attention(*{**PROMPT, **over}.values())
         sd2.kv8_attention(_cache(), *{**ATTEND, **over}.values())
+
+
+def test_largest_counts_as_the_header_has_them():
+    """Sequences up to 65536 and rows up to 2^24, in every call; one more is refused."""
+    wide = _cache(n_slots=65536, n_kv=1)
+    for n_seq, n_rows in ((65536, 0), (0, 1 << 24)):
+        sd2.kv8_append(wide, *{**APPEND, "n_seq": n_seq, "n_rows": n_rows}.values())
+        sd2.prompt_attention(*{**PROMPT, "n_seq": n_seq, "n_rows": n_rows}.values())
+        sd2.kv8_attention(wide, *{**ATTEND, "n_seq": n_seq, "n_rows": n_rows}.values())
+    for over in (dict(n_seq=65537), dict(n_rows=(1 << 24) + 1)):
+        assert _status(sd2.kv8_append, wide, *{**APPEND, **over}.values()) == RANGE
+        assert _status(sd2.prompt_attention, *{**PROMPT, **over}.values()) == RANGE
+        assert _status(sd2.kv8_attention, wide, *{**ATTEND, **over}.values()) == RANGE
+    with open(os.path.join(os.path.dirname(__file__), "..", "include", "sd2.h")) as f:
+        assert "n_seq (0 .. 65536) and n_rows (0 .. 2^24)" in f.read()

@@ -579,3 +579,44 @@ def test_more_workgroups_than_a_grid_dimension_has_threads():
     del slots, want, q, out
     torch.cuda.empty_cache()
     assert same
+
+
+@pytest.mark.parametrize("again", [3, 4])  # four wavefronts a row join in one launch, one in the other
+def test_records_that_nobody_wrote_are_not_followed_past_the_workspace(again):
+    """Sequences that share rows 0 .. 63, so that there are more units of work than the rows allow and the last ones are left out: those of
+    the last 16 tokens of the last sequence.  The joining launch finds in their records what the workspace held before."""
+    n_heads, dim, max_pos, max_new, n_rows = 4, 64, 2048, 64, 128
+    offsets = [0, 64] * again + [64, 128]
+    n_seq = len(offsets) - 1
+    slots = Slots(n_seq, 1, max_pos, dim)
+    for t, x in ((slots.k, 0), (slots.v, 0), (slots.ks, 1.0), (slots.vs, 1.0)):
+        t.fill_(x)
+    nb, guard = sd2.kv8_attention_workspace_size(slots.c, n_heads, n_seq, max_new), 4096
+    records = n_seq * max_new * n_heads
+    slot = 64 * (dim * 4 + 8)  # of a unit: 64 rows of sums, each with its maximum and sum of weights
+    bound = (nb - 16 * records) // slot
+    assert bound * slot == nb - 16 * records
+    # 16 spans of 128 positions for each of 4 row tiles a sequence: one workgroup each, as far as the rows allow
+    run, units = 16 * (n_rows * n_heads // 64 + n_seq), 16 * 4 * (again + 1)
+    assert units - 16 <= bound and units - 64 <= run <= units - 16
+    rest = 1 << 31
+    cases = [((bound - 4, 4, 0), True), ((bound - 4, 5, 0), False), ((bound, 2, 0), False), ((0xFFFFFFFF, 2, 0), False), ((2, rest - 1, 0), False),
+             ((bound - 4, rest | 3, bound - 1), True), ((bound - 4, rest | 3, bound), False), ((bound - 4, rest | 3, 0xFFFFFFFF), False),
+             ((bound - 1, 1, 0), False), ((bound - 1, 0, 0), False), ((bound - 1, rest | 1, bound - 2), True), ((bound - 2, 2, 0xFFFFFFFF), True)]
+    held = np.full(nb + 2 * guard, 0xAB, dtype=np.uint8)
+    inside = held[guard:-guard]
+    inside[:bound * 64 * dim * 4].view(np.float32)[:] = 3.0
+    inside[bound * 64 * dim * 4:-16 * records].view(np.float32).reshape(-1, 2)[:] = [0.0, 1.0]
+    table = inside[-16 * records:].view(np.uint32).reshape(n_seq, max_new, n_heads, 4)
+    table[:] = 0
+    for i, (record, _) in enumerate(cases):
+        table[-1, 48 + i, :, :3] = record
+    ws = torch.from_numpy(held).cuda()
+    q = torch.ones((n_rows + 4, n_heads * dim), dtype=torch.bfloat16, device="cuda")
+    out, rs, p0 = torch.full_like(q, 7.0), i32(offsets), i32([max_pos - 64] * n_seq)
+    sd2.kv8_attention(slots.c, q.data_ptr(), q.stride(0), n_heads, rs.data_ptr(), p0.data_ptr(), n_seq, n_rows, max_new, out.data_ptr(),
+                      ws.data_ptr() + guard, nb, gu.stream_ptr())
+    torch.cuda.synchronize()
+    assert (ws[:guard] == 0xAB).all() and (ws[-guard:] == 0xAB).all() and (out[n_rows:] == 7.0).all()
+    for i, (record, followed) in enumerate(cases):  # sums of a workspace are held at 2^-8 of their size
+        assert (out[64 + 48 + i] == (3.0 * 256 if followed else 7.0)).all(), record

@@ -282,13 +282,17 @@ int sd2_sparse_drafter_decode(const sd2_model_t* model, const uint16_t* h_in_bf1
  *   sd2_sparse_linear (q|k|v) -> sd2_kv8_append -> sd2_prompt_attention (whole prompts) or sd2_kv8_attention (single tokens,
  *   drafts and chunks against the cache) -> sd2_sparse_linear (o).
  * Same decoder as sd2_sparse_drafter_decode: half-split rotary embedding, n_heads / n_kv query heads for each key/value head,
- * scores times 1/sqrt(head_dim), softmax; a position's keys and values are read back as the cache holds them.
+ * scores times 1/sqrt(head_dim), softmax; a position's keys and values are read back as the cache holds them.  Not the same
+ * precision: that call keeps queries and softmax weights in fp32, here queries are bf16 and weights are rounded to bf16 for the product with
+ * the values (against 64 bits 0.0021 of a result's norm, where the rounding of the result alone is 0.0016).
  *
  * Packed rows: the rows of all sequences of a call stand one behind the other; sequence b owns rows row_start_dev[b] ..
  * row_start_dev[b + 1] - 1 (device int32 [n_seq + 1], from 0 on, not decreasing, at most n_rows; a sequence may have none).
  * Rows behind the last sequence's are neither read nor written.  pos0_dev (device int32 [n_seq]): the position of a
  * sequence's first row.  Both are read by the kernels, not by the host: a captured call serves whatever they hold when it is
  * replayed.  Values outside these rules give unspecified results, but no access outside the buffers.
+ * The same call gives the same bits.  In what order sums are added goes by all lengths and counts of a call: the attention of a
+ * sequence may differ in its last bits when it stands alone, among others, or with another n_rows, n_seq or max_pos.
  * n_seq (0 .. 65536) and n_rows (0 .. 2^24) say how large the arrays are; n_rows * n_heads <= 2^30.  With no rows a call does nothing.
  * Outputs must not overlap inputs.
  *
@@ -315,7 +319,11 @@ int sd2_kv8_cache_init(sd2_kv8_cache_t* cache, uint8_t* k_dev, uint8_t* v_dev, f
  * are rotated (angle position * rope_theta^(-2 i / head_dim), computed in 64 bits; rope_theta > 1), all is rounded to bf16 and written
  * to rows_bf16_dev (same layout); the rounded keys and values go into the cache at their positions.  Rows at positions
  * outside 0 .. max_pos - 1 are rounded but not stored.  n_seq <= n_slots.  Positions of a slot from the last new row on keep their
- * codes; what the block of a sequence's first row holds in front of it counts as the sequence's own. */
+ * codes; what the block of a sequence's first row holds in front of it counts as the sequence's own.
+ * Tokens that are taken back later -- drafts that a verification rejects -- are written over by a call at an earlier position, but where they
+ * raised the scale of the block that accepted positions share with them, it stays, and those positions' codes stay rounded to it: at most half a
+ * step of the larger scale.  A program that wants the codes as they were keeps the open block (its 32 positions and scale of each head) from
+ * before the call. */
 int sd2_kv8_append(const sd2_kv8_cache_t* cache, const float* qkv_dev, int32_t n_heads, const int32_t* row_start_dev,
                    const int32_t* pos0_dev, int32_t n_seq, int32_t n_rows, double rope_theta, uint16_t* rows_bf16_dev, void* stream);
 
@@ -323,7 +331,8 @@ int sd2_kv8_append(const sd2_kv8_cache_t* cache, const float* qkv_dev, int32_t n
  * q_dev, k_dev, v_dev: bf16, row r of head h at [r * stride + h * head_dim]; q_stride >= n_heads * head_dim, kv_stride >= n_kv * head_dim,
  * multiples of 8, at most 2^24 (the three may lie in one array, as sd2_kv8_append leaves them).  out_bf16_dev: bf16
  * [n_rows][n_heads * head_dim], what the output linear takes.  fp32 scores, maxima, sums and results; weights are rounded to bf16.
- * Infinities and NaN reach the rows that attend to them and no others. */
+ * Infinities and NaN reach the rows that attend to them and no others.  Results are sums of values times weights of up to 2^8, divided
+ * at the end: rows that attend to n positions are safe from overflow for values up to 2^119 / n, rows over the cache up to 2^127 / n. */
 int sd2_prompt_attention(const uint16_t* q_dev, const uint16_t* k_dev, const uint16_t* v_dev, int64_t q_stride, int64_t kv_stride,
                          const int32_t* row_start_dev, int32_t n_seq, int32_t n_rows, int32_t n_heads, int32_t n_kv, int32_t head_dim,
                          uint16_t* out_bf16_dev, void* stream);
@@ -331,8 +340,9 @@ int sd2_prompt_attention(const uint16_t* q_dev, const uint16_t* k_dev, const uin
 /* Attention of new rows over the cache, theirs included (append them first): row i of sequence b attends to positions
  * 0 .. pos0[b] + i of slot b (positions from max_pos on do not exist; a row at a negative position attends to nothing and its result is
  * zero).  q_dev, q_stride, out_bf16_dev, arithmetic: as for sd2_prompt_attention.  max_new (1 .. 64): the most rows that a sequence
- * has; of a sequence with more, the first max_new are computed.  n_seq <= n_slots, n_seq * max_new * n_heads <= 2^30.  A long history is cut into stretches that
- * workgroups take side by side; workspace_dev (>= the reported size, contents irrelevant before and after) holds their results. */
+ * has; of a sequence with more, the first max_new are computed.  n_seq <= n_slots, n_seq * max_new * n_heads <= 2^30.
+ * A long history is cut into stretches that workgroups take side by side; workspace_dev (>= the reported size, contents irrelevant
+ * before and after) holds their results.  It is asked for whatever the lengths are: the host does not know them. */
 int sd2_kv8_attention_workspace_size(const sd2_kv8_cache_t* cache, int32_t n_heads, int32_t n_seq, int32_t max_new, size_t* bytes_out);
 int sd2_kv8_attention(const sd2_kv8_cache_t* cache, const uint16_t* q_dev, int64_t q_stride, int32_t n_heads,
                       const int32_t* row_start_dev, const int32_t* pos0_dev, int32_t n_seq, int32_t n_rows, int32_t max_new,

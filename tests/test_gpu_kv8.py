@@ -620,3 +620,21 @@ def test_records_that_nobody_wrote_are_not_followed_past_the_workspace(again):
     assert (ws[:guard] == 0xAB).all() and (ws[-guard:] == 0xAB).all() and (out[n_rows:] == 7.0).all()
     for i, (record, followed) in enumerate(cases):  # sums of a workspace are held at 2^-8 of their size
         assert (out[64 + 48 + i] == (3.0 * 256 if followed else 7.0)).all(), record
+
+
+@pytest.mark.parametrize("dim", [64, 128, 256])
+@pytest.mark.parametrize("max_pos,n", [(320, 300), (2048, 2000)])  # taken whole (heads of 256: cut); cut and joined
+def test_values_as_large_as_sums_of_weighted_values_allow(dim, max_pos, n):
+    """Values of one sign just below 2^127 / n under scores that rise by 7.5 powers of two, which the running maximum need not follow."""
+    slots, x = Slots(1, 1, max_pos, dim), torch.zeros(n, 3 * dim, device="cuda")
+    x[:, 2 * dim:] = torch.rand(n, dim, generator=torch.Generator().manual_seed(83)).cuda() * (2.0 ** 127 / n) * 0.9  # codes round up by 1/16
+    append(slots, x, 1, [n], [0])
+    # keys as they are to be, in place of rotated ones
+    slots.k.zero_()
+    slots.k[0, 0, :n, 0] = (torch.arange(n, device="cuda") * (7.5 / n * 32)).to(torch.float8_e4m3fn).view(torch.uint8)
+    slots.ks.fill_(1.0)
+    q = torch.zeros(3, dim, dtype=torch.bfloat16, device="cuda")
+    q[:, 0] = np.log(2.0) * dim ** 0.5 / 32
+    k, v, ks, vs = slots.host()
+    k, v = [kv8.values(k[0], ks[0])], [kv8.values(v[0], vs[0])]
+    check_attention(attend(slots, q, 1, [2], [n - 2], n_rows=2), q, k, v, 1, [2], [n - 2], dim)

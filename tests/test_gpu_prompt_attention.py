@@ -267,3 +267,14 @@ def test_more_workgroups_than_a_grid_dimension_has_threads(n_heads, n_kv):
     del q, k, v, out
     torch.cuda.empty_cache()
     assert same
+
+
+@pytest.mark.parametrize("dim", [64, 128, 256])
+@pytest.mark.parametrize("n,n_heads,n_kv", [(300, 4, 2), (1024, 48, 16)])  # teams of a wavefront; of four
+def test_values_as_large_as_sums_of_weighted_values_allow(dim, n, n_heads, n_kv):
+    """Values of one sign just below 2^119 / n under scores that rise by 7.5 powers of two, which the running maximum need not follow."""
+    q, k, v = torch.zeros(n, n_heads * dim), torch.zeros(n, n_kv * dim), rows(71, n, n_kv, dim)
+    q[:, ::dim], k[:, ::dim] = 1.0, (torch.arange(n) * (7.5 / n * np.log(2.0) * dim ** 0.5))[:, None]
+    q, k = (t.to(torch.bfloat16).cuda() for t in (q, k))
+    v = (v.float().sigmoid() * (2.0 ** 119 / n)).to(torch.bfloat16)
+    check(run(q, k, v, [n], n_heads, n_kv, dim), q, k, v, [n], n_heads, n_kv, dim)

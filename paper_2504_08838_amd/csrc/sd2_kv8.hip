@@ -220,18 +220,18 @@ hipError_t launch_kv8_append(const Kv8Args& c, const float* qkv, int n_heads, co
 // memory straight into LDS, one ahead of the one at work, and values leave it by the transposing read.  Weights are rounded to bf16 for
 // the second product, at most 2^-8 of a weight.
 //
-// Bound by bytes where there are many positions: 59 requests with 226 000 positions in 16 heads of keys and values of 128 (464 MB) 95 us,
+// Bound by bytes where there are many positions: 60 requests with 224 802 positions in 16 heads of keys and values of 128 (464 MB) 95 us,
 // 4.9 TB/s, where a pure read has 5.35 (and 5 us to join); by the chain plan - first tile - scores - meeting (- join) where there are few:
-// one token against 429 positions 6.8 us, five against 30016 15 us.  64 tokens with four query heads a group: 1.9 us for 128 positions of
-// 64 rows, softmax and conversions on the vector ALU.
+// one token against 429 positions 6.7 us (8.1 in a cache of 8192, which is cut), five against 30016 15 us.  64 tokens with four query heads a
+// group: 1.9 us for 128 positions of 64 rows, softmax and conversions on the vector ALU.
 constexpr int kCutWaves = 4, kWholeWaves = 8;  // wavefronts of a workgroup that takes a stretch, and of one that takes all positions
 constexpr int kAttSpan = 32 * kCutWaves;        // positions of four tiles side by side: what stretches are made of
 
 constexpr uint32_t kRest = 0x80000000u;
 
-// Values enter the second product at 2^-8 of their size, and results are multiplied by 2^8 at the end.  The largest that is
-// stored is 256 * 2^120, more than bf16 and fp32 have: as an infinity, it would be NaN in the rows whose weight for it is zero.  The smallest, 2^-109,
-// stays a normal number.
+// Values enter the second product at 2^-8 of their size, and results are multiplied by 2^8 at the end.  The largest that is stored is
+// 256 * 2^120, more than bf16 and fp32 have: as an infinity, it would be NaN in the rows whose weight for it is zero.  The smallest,
+// 2^-109, stays a normal number.
 constexpr float kValuesIn = 0x1p-8f, kResultsOut = 0x1p8f;
 
 struct Kv8AttArgs {
@@ -269,7 +269,7 @@ __device__ __forceinline__ SeqCut seq_cut(const Kv8AttArgs& a, const SeqRows& r)
 // Spans of a stretch, the same for all sequences.  With few row tiles: as few spans as let all stretches run side by side (64 rows against
 // 500 to 4000 positions, four sequences: 24 us with 512 stretches for 512 places, 26 with 448, 32 with 320 and with 832).  With many, twice
 // as many stretches as places, whole ones first and what is left of each sequence behind them: sequences differ in length, and the short
-// ones fill the gaps (59 sequences of 14 to 16000 positions: 101 us; 114 with a stretch a place, 103 with three; 103 with two in the
+// ones fill the gaps (60 sequences of 19 to 16005 positions: 101 us; 114 with a stretch a place, 103 with three; 103 with two in the
 // sequences' order).  A sequence of more than 128 spans is not cut into single ones, as what they leave has to be joined (30000
 // positions: 17.6 us cut into single spans, 14.8 into pairs).
 template <int ROWS>

@@ -12,12 +12,14 @@
 // Keys and values go from memory into LDS without passing through registers, a tile ahead; their 16-byte pieces are turned within a row
 // by the row's number, which spreads the reads over the banks (no conflicts counted).
 //
-// What bounds it: on long prompts the power that products, exponentials and LDS reads draw together -- 8192 tokens, 24 query heads over 8 of
-// 128 dimensions: 397 us, 1040 TFLOP/s, where a library product of 8192^3 reaches 1245; the matrix cores are busy 53 % of 752 000 cycles at
-// 1.9 of 2.4 GHz.  Scores of the next tile made beside the weights of this one: 8 % fewer cycles at a clock 5 % lower, 3 % less time here and
-// 2 to 5 % more for shorter prompts; not kept.  With heads of 64
-// dimensions the exponentials count twice (3001 + 1 + 2500 + 777 tokens, 32 heads: 82 us, 790 TFLOP/s).  On short ones the chain of steps of
-// the last rows, 1.1 us for 64 positions: 300 tokens 8.1 us, 37 tokens 5.9 us, of which a launch that does nothing has 2.
+// What bounds it: on long prompts matrix cores and vector ALU in turn, at a clock that the power they draw sets -- 8192 tokens, 24 query heads
+// over 8 of 128 dimensions: 396 us, 1040 TFLOP/s, where a library product of 8192^3 reaches 1245; the matrix cores are busy 52 % of 768 000
+// cycles, the vector ALU about as long, at 1.9 of 2.4 GHz.  Scores of the next tile made beside the weights of this one: 8 % fewer cycles at a
+// clock 5 % lower, 3 % less time here and 2 to 5 % more for shorter prompts; not kept.  With heads of 64 dimensions the vector instructions
+// count twice (3001 + 1 + 2500 + 777 tokens, 32 heads: 80 us, 805 TFLOP/s): of six a score, one is the exponential.  Other head sizes do the
+// work of 128 or 256 (3000 tokens, 24 heads over 8: 65 us with heads of 80, 70 with 128; 301 with 144, 234 with 256, where a SIMD has one
+// wavefront and a tile serves 32 rows).  On short prompts the chain of steps of the last rows, 1.1 us for 64 positions: 300 tokens 8.2 us,
+// 37 tokens 5.9 us, of which a launch that does nothing has 2.
 #include <type_traits>
 
 #include "sd2_internal.h"
